@@ -113,6 +113,72 @@ st_status st_rope_apply_qk(void* q_out, const void* q, int32_t n_q_heads, void* 
                            int32_t head_dim, double theta_base, st_dtype dt, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Rotation as models ask for it.  st_rope_spec says which pairs of a head are rotated by which angles:
+ *   rotary_dim r : the leading r dims are rotated, the others pass (0: all of head_dim; a multiple of 16)
+ *   layout       : ST_ROPE_HALF pairs (i, i + r/2), ST_ROPE_INTERLEAVED pairs (2i, 2i + 1), i < r/2
+ *   angle        : position * f_i, f_i = theta_base^(-2i/r), changed for long contexts by `scaling`, s = factor >= 1:
+ *     ST_ROPE_LINEAR  f_i / s                                (position interpolation)
+ *     ST_ROPE_NTK     theta_base * s^(r/(r-2)) as the base
+ *     ST_ROPE_YARN    f_i (1 - g_i) + f_i / s * g_i; g rises from 0 to 1 linearly in i between floor(c(beta_fast)) and
+ *                     ceil(c(beta_slow)) (kept in 0 .. r-1), c(n) = r ln(L / (2 pi n)) / (2 ln theta_base) the pair that
+ *                     turns n times over L = original_positions (arXiv 2309.00071)
+ *   attention_factor a : cos and sin are multiplied by it; 0 selects 0.1 ln(s) + 1 for ST_ROPE_YARN and 1 otherwise.
+ * Fields that the chosen scaling does not name are ignored.  Zero-fill the struct, then set what differs.
+ * Angles are formed and reduced in fp64.
+ * ---------------------------------------------------------------------- */
+enum { ST_ROPE_HALF = 0, ST_ROPE_INTERLEAVED = 1 };
+enum { ST_ROPE_PLAIN = 0, ST_ROPE_LINEAR = 1, ST_ROPE_NTK = 2, ST_ROPE_YARN = 3 };
+typedef struct st_rope_spec {
+    double theta_base;          /* > 0 */
+    double factor;              /* s */
+    double beta_fast;           /* 0: 32 */
+    double beta_slow;           /* 0: 1 */
+    double attention_factor;    /* 0: the default of the scaling */
+    int32_t original_positions; /* L */
+    int32_t rotary_dim;
+    int32_t layout;
+    int32_t scaling;
+} st_rope_spec;
+
+/* ------------------------------------------------------------------------
+ * st_norm_rope_apply_qk -- queries and keys normalised per head and rotated, in one launch: what models that
+ * normalise their heads (Qwen3) do between the projections and the attention.  For every row x of head_dim values
+ *   y = R(position) (x * (mean(x^2) + eps)^(-1/2) * weight),      R as the spec says.
+ *   q, q_out : [n_tokens, n_q_heads, head_dim]; k, k_out: [n_tokens, n_kv_heads, head_dim], dtype dt (ST_BF16 or ST_F32).
+ *              q_stride, k_stride: elements from a token's rows to the next token's in q and k, so that both may be slices of one
+ *              projection's output (a multiple of 16 bytes, at least heads * head_dim); q_out and k_out are dense.
+ *              In place (q_out == q, k_out == k) where the stride is dense; other overlaps of inputs and results are not allowed.
+ *   q_weight, k_weight : [head_dim] of dtype dt, or NULL: that tensor is rotated without being normalised.
+ *   n_kv_heads = 0 (k, k_out, k_weight ignored): the queries alone, as for a decoding step whose key goes through
+ *              st_kv_append_norm_rope.
+ *   positions : int32 [n_tokens], eps >= 0.
+ * fp32 arithmetic (the squares are summed in fp32: values up to 2^60), results rounded once.
+ * ---------------------------------------------------------------------- */
+st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
+                                void* k_out, const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
+                                const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                                const st_rope_spec* spec, st_dtype dt, void* hip_stream);
+
+/* Gradients of st_norm_rope_apply_qk:
+ *   d_q_out, d_k_out : dL/d q_out, dL/d k_out, dense
+ *   q, k, q_stride, k_stride, weights, positions, eps, spec : the forward's (q or k may be NULL where its weight is NULL)
+ *   dq, dk           : dL/dq, dL/dk with token strides dq_stride, dk_stride of their own (slices of the gradient of one
+ *                      projection's output); may be d_q_out / d_k_out (dense) or q / k (same stride) themselves
+ *   dq_weight, dk_weight : fp32 [head_dim] (written: the sum over all rows), or NULL where it is not wanted
+ * workspace: at least st_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; not needed (may be NULL) without
+ * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine.
+ * With n_tokens = 0 the weight gradients are written as 0. */
+size_t st_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
+
+st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_weight, const void* d_q_out,
+                              const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
+                              void* dk, int64_t dk_stride, float* dk_weight, const void* d_k_out,
+                              const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
+                              const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                              const st_rope_spec* spec, st_dtype dt, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * st_plan -- segment tables of one packed batch, replacing the dense additive
  * mask of Eq. 2.  The mask depends only on the training / prefill instance
  * (Appendix E.1), so one plan serves every layer and head.

@@ -12,6 +12,8 @@ ST_F32, ST_BF16, ST_FP8_E4M3 = 0, 1, 2
 ST_SOURCE, ST_REASONING = 0, 1
 ST_TILE_SKIP, ST_TILE_FULL, ST_TILE_PARTIAL = 0, 1, 2
 ST_BLOCK_SS, ST_BLOCK_RS, ST_BLOCK_RR = 0, 1, 2
+ST_ROPE_HALF, ST_ROPE_INTERLEAVED = 0, 1
+ST_ROPE_PLAIN, ST_ROPE_LINEAR, ST_ROPE_NTK, ST_ROPE_YARN = 0, 1, 2, 3
 PAGE = 16
 
 _STATUS_NAMES = {1: "ST_ERR_INVALID_ARG", 2: "ST_ERR_SHAPE", 3: "ST_ERR_LAYOUT", 4: "ST_ERR_CAPACITY",
@@ -56,6 +58,18 @@ class _DualLensStruct(C.Structure):
                 ("max_src_len", C.c_int32), ("max_rsn_len", C.c_int32), ("unit_tokens", C.c_int32)]
 
 
+class RopeSpec(C.Structure):
+    """Which pairs of a head are rotated by which angles (st_rope_spec): RopeSpec(theta_base=1.0e6, scaling=ST_ROPE_YARN, ...)."""
+    _fields_ = [("theta_base", C.c_double), ("factor", C.c_double), ("beta_fast", C.c_double), ("beta_slow", C.c_double),
+                ("attention_factor", C.c_double), ("original_positions", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32),
+                ("scaling", C.c_int32)]
+
+    def __init__(self, theta_base=1.0e6, layout=0, rotary_dim=0, scaling=0, factor=1.0, original_positions=0, beta_fast=0.0, beta_slow=0.0,
+                 attention_factor=0.0):
+        super().__init__(float(theta_base), float(factor), float(beta_fast), float(beta_slow), float(attention_factor), int(original_positions),
+                         int(rotary_dim), int(layout), int(scaling))
+
+
 _lib = None
 
 
@@ -92,6 +106,13 @@ def load_library():
     lib.st_rope_apply.argtypes = [vp, vp, vp, i64, i32, i32, f64, i32, vp]
     lib.st_rope_apply_qk.restype = i32
     lib.st_rope_apply_qk.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i32, f64, i32, vp]
+    spec = C.POINTER(RopeSpec)
+    lib.st_norm_rope_apply_qk.restype = i32
+    lib.st_norm_rope_apply_qk.argtypes = [vp, vp, i64, i32, vp, vp, vp, i64, i32, vp, vp, i64, i32, f32, spec, i32, vp]
+    lib.st_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.st_norm_rope_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.st_norm_rope_bwd_qk.restype = i32
+    lib.st_norm_rope_bwd_qk.argtypes = 2 * [vp, i64, vp, vp, vp, i64, i32, vp] + [vp, i64, i32, f32, spec, i32, vp, sz, vp]
     lib.st_plan_workspace_bytes.restype = sz
     lib.st_plan_workspace_bytes.argtypes = [i32, i64]
     lib.st_plan_create.restype = i32
@@ -294,6 +315,86 @@ def st_rope_apply_qk(q, k, positions, theta_base=1.0e6, q_out=None, k_out=None, 
     _check(lib.st_rope_apply_qk(_ptr(q_out), _ptr(q), hq, _ptr(k_out), _ptr(k), k.shape[1], _ptr(positions), n, d, float(theta_base),
                                 _dtype_code(q), _stream(stream)))
     return q_out, k_out
+
+
+# ------------------------------------------------------- norm and rotation --
+def _token_rows(t, name, dtype=None):
+    """Token stride of t[n_tokens, heads, D], whose heads and dims are dense (a slice of a projection's output or a tensor of its own)."""
+    n, h, d = t.shape
+    if not t.is_cuda or (dtype is not None and t.dtype != dtype) or (h > 1 and t.stride(1) != d) or t.stride(2) != 1:
+        raise TypeError(f"{name} must be a device tensor [n_tokens, heads, head_dim] with dense heads, all tensors of one dtype")
+    return t.stride(0) if n > 1 else h * d
+
+
+def _norm_weight(w, x, name):
+    if w is not None and (not w.is_cuda or w.dtype != x.dtype or tuple(w.shape) != (x.shape[2],) or not w.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous device tensor [head_dim] of the rows' dtype")
+    return w
+
+
+def st_norm_rope_apply_qk(q, k, q_weight, k_weight, positions, spec, eps=1.0e-6, q_out=None, k_out=None, stream=None):
+    """q[n_tokens, Hq, D], k[n_tokens, Hkv, D] (or None) normalised per head (weights [D]; None: not normalised) and rotated by
+    positions[n_tokens] as `spec` (RopeSpec) says -> (q_out, k_out).  q and k may be slices of one projection's output; outs default
+    to new dense tensors."""
+    lib = load_library()
+    n, hq, d = q.shape
+    _dev_i32(positions, "positions")
+    assert positions.numel() == n
+    outs, args = [], []
+    for x, w, out, name in ((q, q_weight, q_out, "q"), (k, k_weight, k_out, "k")):
+        if x is None:
+            outs.append(None)
+            args += [None, None, 0, 0, None]
+            continue
+        assert x.shape[0] == n and x.shape[2] == d
+        stride = _token_rows(x, name, q.dtype)
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        assert out.is_cuda and out.shape == x.shape and out.dtype == x.dtype and out.is_contiguous()
+        outs.append(out)
+        args += [_ptr(out), _ptr(x), stride, x.shape[1], _ptr(_norm_weight(w, x, name + "_weight"))]
+    _check(lib.st_norm_rope_apply_qk(*args, _ptr(positions), n, d, float(eps), C.byref(spec), _dtype_code(q), _stream(stream)))
+    return tuple(outs)
+
+
+def st_norm_rope_bwd_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, head_dim):
+    return int(load_library().st_norm_rope_bwd_workspace_bytes(int(n_tokens), n_q_heads, n_kv_heads, head_dim))
+
+
+def st_norm_rope_bwd_qk(d_q_out, d_k_out, q, k, q_weight, k_weight, positions, spec, eps=1.0e-6, dq=None, dk=None, weight_grads=True,
+                        workspace=None, stream=None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of st_norm_rope_apply_qk; the weights' are fp32 [D], None without a weight or
+    with weight_grads=False.  dq and dk may be slices of one gradient; a tensor without a weight may be None (as may k and d_k_out
+    together: the queries alone)."""
+    lib = load_library()
+    n, hq, d = d_q_out.shape
+    _dev_i32(positions, "positions")
+    assert positions.numel() == n
+    grads, sums, args = [], [], []
+    for g, x, w, dx, name in ((d_q_out, q, q_weight, dq, "q"), (d_k_out, k, k_weight, dk, "k")):
+        if g is None:
+            grads.append(None)
+            sums.append(None)
+            args += [None, 0, None, None, None, 0, 0, None]
+            continue
+        assert g.is_cuda and g.is_contiguous() and g.dtype == d_q_out.dtype and g.shape[0] == n and g.shape[2] == d
+        _norm_weight(w, g, name + "_weight")
+        stride = 0
+        if x is not None:
+            assert x.shape == g.shape
+            stride = _token_rows(x, name, g.dtype)
+        if dx is None:
+            dx = torch.empty(g.shape, dtype=g.dtype, device=g.device)
+        assert dx.shape == g.shape
+        dw = torch.empty(d, dtype=torch.float32, device=g.device) if w is not None and weight_grads else None
+        grads.append(dx)
+        sums.append(dw)
+        args += [_ptr(dx), _token_rows(dx, "d" + name, g.dtype), _ptr(dw), _ptr(g), _ptr(x), stride, g.shape[1], _ptr(w)]
+    if workspace is None and any(s is not None for s in sums):
+        workspace = _temp_workspace(st_norm_rope_bwd_workspace_bytes(n, hq, 0 if d_k_out is None else d_k_out.shape[1], d), d_q_out.device, stream)
+    _check(lib.st_norm_rope_bwd_qk(*args, _ptr(positions), n, d, float(eps), C.byref(spec), _dtype_code(d_q_out), _ptr(workspace),
+                                   0 if workspace is None else workspace.nbytes, _stream(stream)))
+    return (*grads, *sums)
 
 
 # ------------------------------------------------------------------ plan --
