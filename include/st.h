@@ -43,9 +43,10 @@ typedef enum st_status {
     ST_ERR_RUNTIME = 6       /* a HIP call failed; text in st_last_error() */
 } st_status;
 
-/* ST_FP8_E4M3 (OCP FP8 E4M3: bias 7, largest value 448, no infinities) names a STORAGE format of the
- * KV caches only; activations are ST_BF16 or ST_F32. */
-typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_FP8_E4M3 = 2 } st_dtype;
+/* ST_FP8_E4M3 (OCP FP8 E4M3: bias 7, largest value 448, no infinities) and ST_MXFP4 (OCP MX: 4-bit E2M1
+ * codes, one E8M0 scale per 32 values) name STORAGE formats of the KV caches only; activations are
+ * ST_BF16 or ST_F32. */
+typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_FP8_E4M3 = 2, ST_MXFP4 = 3 } st_dtype;
 
 /* The two streams of the method; also the value set of stream_ids[]. */
 typedef enum st_stream_kind { ST_SOURCE = 0, ST_REASONING = 1 } st_stream_kind;
@@ -156,7 +157,7 @@ typedef struct st_rope_spec {
  * ---------------------------------------------------------------------- */
 st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
                                 void* k_out, const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
-                                const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                                const int32_t* positions, int64_t n_tokens, int32_t head_dim, double eps,
                                 const st_rope_spec* spec, st_dtype dt, void* hip_stream);
 
 /* Gradients of st_norm_rope_apply_qk:
@@ -174,7 +175,7 @@ st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_weight, con
                               const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
                               void* dk, int64_t dk_stride, float* dk_weight, const void* d_k_out,
                               const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
-                              const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                              const int32_t* positions, int64_t n_tokens, int32_t head_dim, double eps,
                               const st_rope_spec* spec, st_dtype dt, void* workspace, size_t workspace_bytes,
                               void* hip_stream);
 
@@ -380,8 +381,23 @@ st_status st_attn_prefill_bwd(void* dq, void* dk, void* dv, const void* d_out, c
  *   v_pool  : [n_pages][n_kv_heads][head_dim][16 slots]
  *   k_scale, v_scale : fp32 [n_pages][n_kv_heads][16 slots]
  * st_kv_append (bf16 rows in, quantised on the way) and st_attn_decode_dual(_rope) with
- * q_len * (n_q_heads / n_kv_heads) <= 16 accept them; every other call that takes a cache gives
- * ST_ERR_UNSUPPORTED.  Both caches of a pair must have the same dtype.
+ * q_len * (n_q_heads / n_kv_heads) <= 16 accept them, as do st_kv_append_norm_rope and st_kv_read; every
+ * other call that takes a cache gives ST_ERR_UNSUPPORTED.  Both caches of a pair must have the same dtype.
+ *
+ * 4-bit caches (dtype = ST_MXFP4; a storage variant, not in the paper): every block of 32 dims of a row -- one
+ * token of one KV head, keys and values separately -- is stored as E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives: codes 0 .. 7 and 8 .. 15) of the block divided by a power of two 2^k, k the smallest integer (not below
+ * -100) for which the block's largest magnitude is at most 6 * 2^k, with the byte k + 127 beside it (k = 0 for an all-zero
+ * block).  The division is exact, the rounding is to nearest, ties to the even code.  A block with an infinite or undefined
+ * element has scale byte 255 and reads as NaN as a whole; values of 2^127 and above may read as infinite.
+ * 4.25 bits per element.  Layouts, in bytes, chosen so that one 16-byte load per lane is a matrix-core operand:
+ *   k_pool : [n_pages][n_kv_heads][head_dim / 32][16 slots][16]    element (page,h,slot,d) is nibble d % 2 of byte (d % 32) / 2
+ *   v_pool : [n_pages][n_kv_heads][4][16][head_dim / 32][4]        element (page,h,slot,d) is nibble (d / 16) % 2 of byte
+ *            [slot / 4][d % 16][d / 32][slot % 4]
+ *   k_scale: bytes [n_pages][n_kv_heads][head_dim], the scales of keys AND values (cast to float*; v_scale is not used):
+ *            [head_dim / 32][16 slots] of the keys, then [slot / 4][head_dim / 32][slot % 4] of the values
+ * st_kv_append, st_kv_append_rope, st_kv_append_norm_rope, st_kv_read and st_attn_decode_dual(_rope, _static) accept
+ * them; every other call that takes a cache gives ST_ERR_UNSUPPORTED.
  * ---------------------------------------------------------------------- */
 typedef struct st_kv_cache {
     void* k_pool;
@@ -393,8 +409,8 @@ typedef struct st_kv_cache {
     int32_t page_size;         /* must be 16 */
     int32_t n_kv_heads;
     int32_t head_dim;
-    int32_t dtype;             /* st_dtype of the pools: ST_BF16 or ST_FP8_E4M3 */
-    float* k_scale;            /* ST_FP8_E4M3 only (NULL otherwise): row scales, see above */
+    int32_t dtype;             /* st_dtype of the pools: ST_BF16, ST_FP8_E4M3 or ST_MXFP4 */
+    float* k_scale;            /* ST_FP8_E4M3: row scales; ST_MXFP4: k_scale holds all scale bytes; else NULL, see above */
     float* v_scale;
 } st_kv_cache;
 
@@ -443,6 +459,40 @@ st_status st_kv_append_rope(const st_dual_cache* caches, st_stream_kind which,
                             double theta_base, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * st_kv_append_norm_rope -- new tokens straight from the projections into a cache of ANY storage format: their keys are
+ * normalised per head and rotated (as by st_norm_rope_apply_qk, position id = index in this cache), keys and values are coded if
+ * the format asks for it, and stored; one launch.
+ *
+ *   k_new, v_new : bf16, token i of sequence b at element (b * max_new + i) * k_stride (v_stride), [n_kv_heads, head_dim]
+ *                  dense there: slices of one projection's output are fine.  Strides are multiples of 8.
+ *   start_len    : device int32 [batch], the index of each sequence's first new token; or NULL for the cache's
+ *                  appended_len (then the call takes a second, tiny launch unless max_new is 1).  Given, it is authoritative: the tokens are stored at
+ *                  start_len[b] .. and appended_len[b] becomes start_len[b] + n_new[b], so a caller can go back
+ *                  to an earlier length (rejected drafts) and append there in one call; max_new = 0 sets the lengths alone.
+ *   n_new, max_new, batch, host_len_upper_bound, page tables, what is dropped: as for st_kv_append (the bound is on
+ *                  start + n_new)
+ *   k_weight     : bf16 [head_dim], or NULL: keys are not normalised.  eps >= 0.
+ *   spec         : or NULL: keys are not rotated.
+ * Keys are normalised and rotated in fp64 and rounded to bf16 once; codes are formed from those bf16 rows.
+ * ---------------------------------------------------------------------- */
+st_status st_kv_append_norm_rope(const st_dual_cache* caches, st_stream_kind which,
+                                 const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                 const int32_t* start_len, const int32_t* n_new, int32_t max_new, int32_t batch,
+                                 int32_t host_len_upper_bound, const void* k_weight, double eps,
+                                 const st_rope_spec* spec, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * st_kv_read -- rows of a cache of any storage format as bf16 (the values that the codes stand for, exactly):
+ * tokens first[b] .. first[b] + n[b] - 1 of every sequence, as when a cache of codes is moved into another, or its tokens go
+ * through the prefill attention again.
+ *   k_out, v_out : bf16 [batch, max_n, n_kv_heads, head_dim], token first[b] + i in row i.  Rows from n[b] on, tokens past the page
+ *                  table and tokens whose page id is outside the pool are left as they were.
+ *   first, n     : device int32 [batch]; NULL for 0 and for max_n
+ * ---------------------------------------------------------------------- */
+st_status st_kv_read(const st_dual_cache* caches, st_stream_kind which, void* k_out, void* v_out, const int32_t* first,
+                     const int32_t* n, int32_t max_n, int32_t batch, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * st_attn_decode_dual -- one decode step over both caches.  Alg. 1: the slice of
  * the source cache that keeps N_EOS == N_EOT + 1 and the reasoning cache are read
  * as one merged cache.  Here nothing is copied: partial softmaxes over chunks of
@@ -457,6 +507,7 @@ st_status st_kv_append_rope(const st_dual_cache* caches, st_stream_kind which,
  *                        (they are appended first); row t of q_len sees reasoning
  *                        tokens [0, rsn_len - q_len + t]
  *   q_len * (n_q_heads / n_kv_heads) must be <= 32.
+ *   Codes of 8-bit and 4-bit caches are read as the values they stand for.
  *   max_src_len / max_rsn_len : host upper bounds on the two length vectors (grid size).
  * A row that sees nothing (both lengths 0) gets out = 0, lse = -inf.  Cache slots
  * outside the visible ranges are never used, whatever bit patterns they hold.

@@ -71,27 +71,24 @@ def bf16(x):
 
 def block_exponent(amax, largest):
     """The smallest k from -100 on with amax <= largest * 2^k; 0 for amax = 0."""
-    k = -100
-    if amax == 0.0:
-        return 0
-    while amax > largest * 2.0 ** k:
-        k += 1
-    return k
+    amax = np.asarray(amax, np.float64)
+    k = np.full(amax.shape, -100)
+    while True:
+        short = amax > largest * np.ldexp(1.0, k)
+        if not short.any():
+            return np.where(amax == 0.0, 0, k)
+        k = k + short
 
 
 def mxfp4(x):
     """What the 4-bit cache holds for rows x[..., D]: the E2M1 values times 2^k of every block of 32 (ties to the even code); a block with an
     infinite or undefined element reads as NaN."""
     y = np.asarray(x, np.float64).reshape(-1, 32)
-    out = np.empty_like(y)
-    for i, block in enumerate(y):
-        if not np.isfinite(block).all():
-            out[i] = np.nan
-            continue
-        k = block_exponent(np.abs(block).max(), 6.0)
-        z = np.abs(block) / 2.0 ** k
-        gap = np.abs(z[:, None] - E2M1)
-        best = gap.min(1, keepdims=True)
-        code = np.array([min(np.nonzero(row)[0], key=lambda c: c % 2) for row in gap == best])
-        out[i] = np.copysign(E2M1[code] * 2.0 ** k, block)
+    bad = ~np.isfinite(y).all(1)
+    y = np.where(bad[:, None], 0.0, y)
+    k = block_exponent(np.abs(y).max(1), 6.0)[:, None]
+    even_first = np.array([0, 2, 4, 6, 1, 3, 5, 7])
+    gap = np.abs(np.ldexp(np.abs(y), -k)[..., None] - E2M1[even_first])
+    out = np.copysign(np.ldexp(E2M1[even_first[gap.argmin(-1)]], k), y)
+    out[bad] = np.nan
     return out.reshape(np.shape(x))

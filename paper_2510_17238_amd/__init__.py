@@ -5,10 +5,10 @@ marshals arguments (torch tensors -> device pointers, the current HIP stream).  
 no CPU or PyTorch fallback: importing the binding without a built library raises.
 """
 from .binding import (  # noqa: F401
-    ST_SOURCE, ST_REASONING, ST_F32, ST_BF16, ST_FP8_E4M3, ST_BLOCK_SS, ST_BLOCK_RS, ST_BLOCK_RR,
+    ST_SOURCE, ST_REASONING, ST_F32, ST_BF16, ST_FP8_E4M3, ST_MXFP4, ST_BLOCK_SS, ST_BLOCK_RS, ST_BLOCK_RR,
     ST_TILE_SKIP, ST_TILE_FULL, ST_TILE_PARTIAL, PAGE,
     ST_ROPE_HALF, ST_ROPE_INTERLEAVED, ST_ROPE_PLAIN, ST_ROPE_LINEAR, ST_ROPE_NTK, ST_ROPE_YARN, RopeSpec,
-    st_norm_rope_apply_qk, st_norm_rope_bwd_workspace_bytes, st_norm_rope_bwd_qk,
+    st_norm_rope_apply_qk, st_norm_rope_bwd_workspace_bytes, st_norm_rope_bwd_qk, st_kv_append_norm_rope, st_kv_read,
     StError, Plan, KVCache, DualCache, library_path, load_library, load_probe_library,
     st_version, st_last_error, st_profile_enable, st_profile_repeat, st_profile_wave_trace, st_profile_read, st_probe_paged_read, st_probe_mfma_bf16, ST_PROF_PREFILL_ATTN, ST_PROF_DECODE_SPLIT, ST_PROF_BWD_DQ, ST_PROF_BWD_DKV, ST_PROF_TILE_PACK, ST_PROF_SOURCE_CHUNK, st_rope_apply, st_rope_apply_qk, st_plan_workspace_bytes, st_plan_create,
     st_prefill_workspace_bytes, st_attn_prefill, st_attn_prefill_rope, st_attn_prefill_ids, st_attn_prefill_bwd, st_kv_append, st_kv_append_rope, st_attn_decode_dual_append, st_decode_workspace_bytes,

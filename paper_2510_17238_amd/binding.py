@@ -8,7 +8,7 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 ST_OK = 0
-ST_F32, ST_BF16, ST_FP8_E4M3 = 0, 1, 2
+ST_F32, ST_BF16, ST_FP8_E4M3, ST_MXFP4 = 0, 1, 2, 3
 ST_SOURCE, ST_REASONING = 0, 1
 ST_TILE_SKIP, ST_TILE_FULL, ST_TILE_PARTIAL = 0, 1, 2
 ST_BLOCK_SS, ST_BLOCK_RS, ST_BLOCK_RR = 0, 1, 2
@@ -108,11 +108,11 @@ def load_library():
     lib.st_rope_apply_qk.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i32, f64, i32, vp]
     spec = C.POINTER(RopeSpec)
     lib.st_norm_rope_apply_qk.restype = i32
-    lib.st_norm_rope_apply_qk.argtypes = [vp, vp, i64, i32, vp, vp, vp, i64, i32, vp, vp, i64, i32, f32, spec, i32, vp]
+    lib.st_norm_rope_apply_qk.argtypes = [vp, vp, i64, i32, vp, vp, vp, i64, i32, vp, vp, i64, i32, f64, spec, i32, vp]
     lib.st_norm_rope_bwd_workspace_bytes.restype = sz
     lib.st_norm_rope_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32]
     lib.st_norm_rope_bwd_qk.restype = i32
-    lib.st_norm_rope_bwd_qk.argtypes = 2 * [vp, i64, vp, vp, vp, i64, i32, vp] + [vp, i64, i32, f32, spec, i32, vp, sz, vp]
+    lib.st_norm_rope_bwd_qk.argtypes = 2 * [vp, i64, vp, vp, vp, i64, i32, vp] + [vp, i64, i32, f64, spec, i32, vp, sz, vp]
     lib.st_plan_workspace_bytes.restype = sz
     lib.st_plan_workspace_bytes.argtypes = [i32, i64]
     lib.st_plan_create.restype = i32
@@ -144,6 +144,10 @@ def load_library():
     lib.st_kv_append.argtypes = [C.POINTER(_DualCacheStruct), i32, vp, vp, vp, i32, i32, i32, vp]
     lib.st_kv_append_rope.restype = i32
     lib.st_kv_append_rope.argtypes = [C.POINTER(_DualCacheStruct), i32, vp, vp, vp, i32, i32, i32, C.c_double, vp]
+    lib.st_kv_append_norm_rope.restype = i32
+    lib.st_kv_append_norm_rope.argtypes = [C.POINTER(_DualCacheStruct), i32, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, f64, spec, vp]
+    lib.st_kv_read.restype = i32
+    lib.st_kv_read.argtypes = [C.POINTER(_DualCacheStruct), i32, vp, vp, vp, vp, i32, i32, vp]
     lib.st_attn_decode_dual_rope.restype = i32
     lib.st_attn_decode_dual_rope.argtypes = [vp, vp, vp, C.POINTER(_DualCacheStruct), C.POINTER(_DualLensStruct), i32, i32,
                                              f32, C.c_double, vp, sz, vp]
@@ -559,10 +563,11 @@ def st_attn_prefill_ids(q, k, v, segment_ids, stream_ids, positions, cu_seqlens,
 class KVCache:
     """Caller-owned paged cache: pools, page table and length vector are torch tensors."""
 
-    def __init__(self, n_pages, batch, max_pages_per_seq, n_kv_heads, head_dim, page_table, device="cuda", fill=None, fp8=False):
+    def __init__(self, n_pages, batch, max_pages_per_seq, n_kv_heads, head_dim, page_table, device="cuda", fill=None, fp8=False, mxfp4=False):
         self.n_pages, self.batch, self.max_pages_per_seq = n_pages, batch, max_pages_per_seq
         self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
-        self.fp8 = bool(fp8)
+        self.fp8, self.mxfp4 = bool(fp8), bool(mxfp4)
+        assert not (self.fp8 and self.mxfp4)
         shape_k = (n_pages, n_kv_heads, head_dim // 8, PAGE, 8)
         shape_v = (n_pages, n_kv_heads, head_dim, PAGE)
         self.k_scale = self.v_scale = None
@@ -572,6 +577,12 @@ class KVCache:
             self.v_pool = torch.full(shape_v, 0 if fill is None else int(fill), dtype=torch.uint8, device=device)
             self.k_scale = torch.full((n_pages, n_kv_heads, PAGE), float("nan") if fill is not None else 0.0, dtype=torch.float32, device=device)
             self.v_scale = self.k_scale.clone()
+        elif self.mxfp4:
+            # E2M1 codes, two a byte, and E8M0 scale bytes of keys and values; `fill` (a byte) pre-sets codes and scales
+            byte = 0 if fill is None else int(fill)
+            self.k_pool = torch.full((n_pages, n_kv_heads, head_dim // 32, PAGE, 16), byte, dtype=torch.uint8, device=device)
+            self.v_pool = torch.full((n_pages, n_kv_heads, 4, 16, head_dim // 32, 4), byte, dtype=torch.uint8, device=device)
+            self.k_scale = torch.full((n_pages, n_kv_heads, head_dim), byte, dtype=torch.uint8, device=device)
         elif fill is None:
             self.k_pool = torch.empty(shape_k, dtype=torch.bfloat16, device=device)
             self.v_pool = torch.empty(shape_v, dtype=torch.bfloat16, device=device)
@@ -585,8 +596,8 @@ class KVCache:
     def struct(self):
         return _KVCacheStruct(self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.page_table.data_ptr(),
                               self.appended_len.data_ptr(), self.max_pages_per_seq, self.n_pages, PAGE,
-                              self.n_kv_heads, self.head_dim, ST_FP8_E4M3 if self.fp8 else ST_BF16,
-                              self.k_scale.data_ptr() if self.fp8 else None, self.v_scale.data_ptr() if self.fp8 else None)
+                              self.n_kv_heads, self.head_dim, ST_FP8_E4M3 if self.fp8 else ST_MXFP4 if self.mxfp4 else ST_BF16,
+                              _ptr(self.k_scale), _ptr(self.v_scale))
 
 
 class DualCache:
@@ -662,6 +673,57 @@ def st_kv_append(caches, which, k_new, v_new, n_new=None, host_len_upper_bound=N
 def st_kv_append_rope(caches, which, k_new, v_new, theta_base, n_new=None, host_len_upper_bound=None, stream=None):
     """st_kv_append for UNROTATED keys: each key is rotated by its index in the cache on the way in."""
     st_kv_append(caches, which, k_new, v_new, n_new, host_len_upper_bound, stream, rope_theta=theta_base)
+
+
+def _batch_rows(t, name, caches):
+    """Token stride of t[batch, tokens, Hkv, D], whose heads and dims are dense and whose sequences lie one behind the other."""
+    b, m, h, d = t.shape
+    if not t.is_cuda or t.dtype != torch.bfloat16 or h != caches.source.n_kv_heads or d != caches.source.head_dim or t.stride(3) != 1 or (h > 1 and t.stride(2) != d):
+        raise TypeError(f"{name} must be a bf16 device tensor [batch, tokens, n_kv_heads, head_dim] with dense heads")
+    stride = t.stride(1) if m > 1 else t.stride(0) if b > 1 and m == 1 else h * d
+    if b > 1 and m > 0 and t.stride(0) != m * stride:
+        raise TypeError(f"{name}: the sequences must lie one behind the other")
+    return stride
+
+
+def st_kv_append_norm_rope(caches, which, k_new, v_new, k_weight, spec, eps=1.0e-6, start_len=None, n_new=None, host_len_upper_bound=None,
+                           stream=None):
+    """k_new, v_new: bf16 [batch, max_new, Hkv, D] (slices of a projection's output are fine) into a cache of any storage format; keys are
+    normalised (k_weight [D] or None) and rotated by their index in the cache (spec: RopeSpec or None).  start_len: int32 [batch]
+    device tensor, where the tokens go (None: behind what is there)."""
+    lib = load_library()
+    batch, max_new = k_new.shape[0], k_new.shape[1]
+    assert k_new.shape == v_new.shape
+    cache = caches.source if which == ST_SOURCE else caches.reasoning
+    assert batch == cache.batch
+    if k_weight is not None and (not k_weight.is_cuda or k_weight.dtype != torch.bfloat16 or tuple(k_weight.shape) != (cache.head_dim,) or not k_weight.is_contiguous()):
+        raise TypeError("k_weight must be a contiguous bf16 device tensor [head_dim]")
+    for t, name in ((start_len, "start_len"), (n_new, "n_new")):
+        if t is not None:
+            assert _dev_i32(t, name).numel() == batch
+    if host_len_upper_bound is None:
+        host_len_upper_bound = cache.max_pages_per_seq * PAGE
+    st = caches.struct()
+    _check(lib.st_kv_append_norm_rope(C.byref(st), which, _ptr(k_new), _batch_rows(k_new, "k_new", caches), _ptr(v_new),
+                                      _batch_rows(v_new, "v_new", caches), _ptr(start_len), _ptr(n_new), max_new, batch,
+                                      int(host_len_upper_bound), _ptr(k_weight), float(eps), None if spec is None else C.byref(spec),
+                                      _stream(stream)))
+
+
+def st_kv_read(caches, which, k_out, v_out, first=None, n=None, stream=None):
+    """Tokens first .. first + n - 1 (int32 [batch] device tensors; None: from 0, all that fit) of every sequence of a cache, as bf16 into
+    k_out, v_out [batch, max_n, Hkv, D]; rows past n are left as they were.  Returns (k_out, v_out)."""
+    lib = load_library()
+    cache = caches.source if which == ST_SOURCE else caches.reasoning
+    for t in (k_out, v_out):
+        assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 4
+        assert t.shape[0] == cache.batch and tuple(t.shape[2:]) == (cache.n_kv_heads, cache.head_dim) and t.shape[1] == k_out.shape[1]
+    for t, name in ((first, "first"), (n, "n")):
+        if t is not None:
+            assert _dev_i32(t, name).numel() == cache.batch
+    st = caches.struct()
+    _check(lib.st_kv_read(C.byref(st), which, _ptr(k_out), _ptr(v_out), _ptr(first), _ptr(n), k_out.shape[1], k_out.shape[0], _stream(stream)))
+    return k_out, v_out
 
 
 def st_decode_workspace_bytes(batch, n_q_heads, n_kv_heads, head_dim, q_len, max_src_len, max_rsn_len, unit_tokens=0):

@@ -11,7 +11,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libst.so")
 PROBE_LIB = os.path.join(HERE, "libst_probe.so")
 
-SOURCES = ["st_error.hip", "st_rope.hip", "st_norm.hip", "st_plan.hip", "st_prefill.hip", "st_prefill_bwd.hip", "st_attn_f32.hip", "st_cache.hip", "st_decode.hip", "st_sched.hip"]
+SOURCES = ["st_error.hip", "st_rope.hip", "st_norm.hip", "st_plan.hip", "st_prefill.hip", "st_prefill_bwd.hip", "st_attn_f32.hip", "st_cache.hip", "st_rows.hip", "st_decode.hip", "st_decode4.hip", "st_sched.hip"]
 PROBE_SOURCES = ["st_probe.hip"]            # (linked with st_error.o for the error text)
 
 FLAGS = [

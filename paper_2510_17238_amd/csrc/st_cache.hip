@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include "st_cache.h"
+#include "st_norm.h"
 
 namespace st {
 
@@ -265,7 +266,7 @@ __global__ void kv_append_bump_kernel(int32_t* __restrict__ appended_len, const 
     appended_len[b] = start + n;
 }
 
-st_status check_cache(const st_kv_cache& c, const char* who, const char* which, bool allow_fp8) {
+st_status check_cache(const st_kv_cache& c, const char* who, const char* which, bool allow_fp8, bool allow_fp4) {
     if (!c.k_pool || !c.v_pool || !c.page_table) return fail(ST_ERR_INVALID_ARG, "%s: %s cache has a null pointer", who, which);
     if (!aligned16(c.k_pool) || !aligned16(c.v_pool)) return fail(ST_ERR_INVALID_ARG, "%s: %s pools must be 16-byte aligned", who, which);
     if (c.page_size != kPage) return fail(ST_ERR_UNSUPPORTED, "%s: page_size %d (must be %d)", who, c.page_size, kPage);
@@ -273,8 +274,11 @@ st_status check_cache(const st_kv_cache& c, const char* who, const char* which, 
         if (!allow_fp8) return fail(ST_ERR_UNSUPPORTED, "%s: 8-bit caches are not supported by this call", who);
         if (!c.k_scale || !c.v_scale) return fail(ST_ERR_INVALID_ARG, "%s: %s cache is ST_FP8_E4M3 but has no scale arrays", who, which);
         if (!aligned16(c.k_scale) || !aligned16(c.v_scale)) return fail(ST_ERR_INVALID_ARG, "%s: %s scale arrays must be 16-byte aligned", who, which);
+    } else if (c.dtype == ST_MXFP4) {
+        if (!allow_fp4) return fail(ST_ERR_UNSUPPORTED, "%s: 4-bit caches are not supported by this call", who);
+        if (!c.k_scale || !aligned16(c.k_scale)) return fail(ST_ERR_INVALID_ARG, "%s: %s cache is ST_MXFP4 and needs a 16-byte aligned scale array", who, which);
     } else if (c.dtype != ST_BF16) {
-        return fail(ST_ERR_UNSUPPORTED, "%s: cache dtype %d (ST_BF16 or ST_FP8_E4M3)", who, c.dtype);
+        return fail(ST_ERR_UNSUPPORTED, "%s: cache dtype %d (ST_BF16, ST_FP8_E4M3 or ST_MXFP4)", who, c.dtype);
     }
     if (c.head_dim != 64 && c.head_dim != 128) return fail(ST_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128)", who, c.head_dim);
     if (c.n_kv_heads <= 0 || c.max_pages_per_seq <= 0 || c.n_pages <= 0) return fail(ST_ERR_INVALID_ARG, "%s: %s cache has non-positive sizes", who, which);
@@ -290,7 +294,7 @@ CacheView cache_view(const st_kv_cache& c) {
     v.max_pages = c.max_pages_per_seq;
     v.n_pages = c.n_pages;
     v.n_kv_heads = c.n_kv_heads;
-    v.k_scale = c.dtype == ST_FP8_E4M3 ? c.k_scale : nullptr;
+    v.k_scale = c.dtype != ST_BF16 ? c.k_scale : nullptr;
     v.v_scale = c.dtype == ST_FP8_E4M3 ? c.v_scale : nullptr;
     return v;
 }
@@ -322,7 +326,7 @@ static st_status kv_append_impl(const char* who, const st_dual_cache* caches, st
     if (!caches || !k_new || !v_new) return fail(ST_ERR_INVALID_ARG, "%s: null pointer", who);
     if (which != ST_SOURCE && which != ST_REASONING) return fail(ST_ERR_INVALID_ARG, "%s: which = %d", who, int(which));
     const st_kv_cache& c = which == ST_SOURCE ? caches->source : caches->reasoning;
-    st_status r = check_cache(c, who, which == ST_SOURCE ? "source" : "reasoning", !rotate);
+    st_status r = check_cache(c, who, which == ST_SOURCE ? "source" : "reasoning", !rotate, true);
     if (r != ST_OK) return r;
     const bool fp8 = c.dtype == ST_FP8_E4M3;
     if (!c.appended_len) return fail(ST_ERR_INVALID_ARG, "%s: appended_len is null", who);
@@ -334,6 +338,18 @@ static st_status kv_append_impl(const char* who, const st_dual_cache* caches, st
                     host_len_upper_bound, (long long)capacity);
     if (rotate && !(theta_base > 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: theta_base must be positive", who);
     if (max_new == 0) return ST_OK;
+    if (c.dtype == ST_MXFP4) {
+        RopeTable rope;
+        if (rotate) {
+            st_rope_spec spec{};
+            spec.theta_base = theta_base;
+            r = make_rope_table(who, &spec, c.head_dim, &rope);
+            if (r != ST_OK) return r;
+        }
+        const int64_t stride = int64_t(c.n_kv_heads) * c.head_dim;
+        return append_rows(who, c, k_new, stride, v_new, stride, nullptr, n_new, max_new, batch, nullptr, 0.0, rotate ? &rope : nullptr,
+                           static_cast<hipStream_t>(hip_stream));
+    }
     const int touched = (max_new + kPage - 1) / kPage + 1;
     const int64_t blocks = int64_t(batch) * c.n_kv_heads * touched;
     if (blocks > 0x7fffffff) return fail(ST_ERR_SHAPE, "%s: grid too large", who);

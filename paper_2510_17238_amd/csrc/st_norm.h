@@ -1,5 +1,7 @@
 // Rotation by a caller's st_rope_spec, and what the kernels that normalise rows share (internal).
 #pragma once
+#include <type_traits>
+
 #include "st_internal.h"
 
 namespace st {
@@ -9,7 +11,7 @@ struct RopeTable {
     double f[64];
     int rot;            // leading dims that are rotated (a multiple of 16)
     int interleaved;    // pairs (2 i, 2 i + 1) instead of (i, i + rot / 2)
-    float a;            // factor on the rotated dims
+    double a;           // factor on the rotated dims
 };
 // Checks the spec and forms the table (ST_OK), or says what is wrong with it.
 st_status make_rope_table(const char* who, const st_rope_spec* spec, int head_dim, RopeTable* table);

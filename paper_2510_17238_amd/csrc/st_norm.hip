@@ -65,7 +65,7 @@ st_status make_rope_table(const char* who, const st_rope_spec* spec, int head_di
     }
     t.rot = rot;
     t.interleaved = s.layout == ST_ROPE_INTERLEAVED;
-    t.a = float(a);
+    t.a = a;
     kept = t;
     kept_spec = s;
     kept_dim = head_dim;
@@ -142,8 +142,8 @@ __device__ __forceinline__ void norm_table(const NormArgs& a, int64_t tok0, int 
         const double rev = double(a.positions[tok0 + t]) * a.rope.f[i] * 0.15915494309189535;        // angle / 2 pi, reduced in 64 bits
         float sn, cs;
         sincosf(float((rev - rint(rev)) * 6.283185307179586), &sn, &cs);
-        s_cos[w] = cs * a.rope.a;
-        s_sin[w] = sn * a.rope.a;
+        s_cos[w] = cs * float(a.rope.a);
+        s_sin[w] = sn * float(a.rope.a);
     }
 }
 
@@ -400,7 +400,7 @@ using namespace st;
 
 extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight, void* k_out,
                                            const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
-                                           const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                                           const int32_t* positions, int64_t n_tokens, int32_t head_dim, double eps,
                                            const st_rope_spec* spec, st_dtype dt, void* hip_stream) {
     const char* who = "st_norm_rope_apply_qk";
     if (dt != ST_F32 && dt != ST_BF16) return fail(ST_ERR_UNSUPPORTED, "%s: dtype %d", who, int(dt));
@@ -409,7 +409,7 @@ extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q
     st_status r = make_rope_table(who, spec, head_dim, &a.rope);
     if (r != ST_OK) return r;
     if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
-    if (!(eps >= 0.f)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    if (!(eps >= 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
     if (n_tokens == 0) return ST_OK;
     if (!positions) return fail(ST_ERR_INVALID_ARG, "%s: positions is null", who);
     const struct { void* out; const void* x; int64_t stride; int heads; const void* w; const char* name; } in[2] = {
@@ -424,7 +424,7 @@ extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q
     }
     a.positions = positions;
     a.n_tokens = n_tokens;
-    a.eps = eps;
+    a.eps = float(eps);
     // Rows of a workgroup: one pass of its threads while that makes no more than 1,024 workgroups, else about four tokens, whose table
     // the heads share.
     const int heads = n_q_heads + n_kv_heads, pass = kNormThreads / (head_dim / 8);
@@ -454,7 +454,7 @@ extern "C" size_t st_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int32_t n_q
 extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_weight, const void* d_q_out, const void* q, int64_t q_stride,
                                          int32_t n_q_heads, const void* q_weight, void* dk, int64_t dk_stride, float* dk_weight,
                                          const void* d_k_out, const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,
-                                         const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                                         const int32_t* positions, int64_t n_tokens, int32_t head_dim, double eps,
                                          const st_rope_spec* spec, st_dtype dt, void* workspace, size_t workspace_bytes, void* hip_stream) {
     const char* who = "st_norm_rope_bwd_qk";
     if (dt != ST_F32 && dt != ST_BF16) return fail(ST_ERR_UNSUPPORTED, "%s: dtype %d", who, int(dt));
@@ -463,7 +463,7 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     st_status r = make_rope_table(who, spec, head_dim, &a.rope);
     if (r != ST_OK) return r;
     if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
-    if (!(eps >= 0.f)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    if (!(eps >= 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
     if (!positions && n_tokens > 0) return fail(ST_ERR_INVALID_ARG, "%s: positions is null", who);
     const struct { void* dx; int64_t dx_stride; float* dw; const void* g; const void* x; int64_t x_stride; int heads; const void* w; const char *name, *dname; } in[2] = {
         {dq, dq_stride, dq_weight, d_q_out, q, q_stride, n_q_heads, q_weight, "q", "dq"},
@@ -496,7 +496,7 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     }
     a.positions = positions;
     a.n_tokens = n_tokens;
-    a.eps = eps;
+    a.eps = float(eps);
     a.tokens = bwd_tokens(n_tokens);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int blocks = bwd_workgroups(n_tokens);

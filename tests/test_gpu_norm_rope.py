@@ -1,11 +1,10 @@
 """Heads normalised and rotated in one pass, and the gradients of that pass, against the formulas in 64 bits."""
-import itertools
-
 import numpy as np
 import pytest
 import torch
 
 from oracle import layer_ops as L
+from rows_helpers import f64, spec_of
 
 DEV = "cuda"
 U24 = 2.0 ** -24
@@ -17,19 +16,6 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 def st():
     import paper_2510_17238_amd as st
     return st
-
-
-def spec_of(st, layout="half", rotary=0, scaling="plain", factor=1.0, original=0, theta=1.0e6, attention=0.0, dim=128):
-    """(library's spec, oracle's (frequencies, factor, layout))."""
-    kinds = {"plain": st.ST_ROPE_PLAIN, "linear": st.ST_ROPE_LINEAR, "ntk": st.ST_ROPE_NTK, "yarn": st.ST_ROPE_YARN}
-    spec = st.RopeSpec(theta_base=theta, layout=st.ST_ROPE_HALF if layout == "half" else st.ST_ROPE_INTERLEAVED, rotary_dim=rotary,
-                       scaling=kinds[scaling], factor=factor, original_positions=original, attention_factor=attention)
-    freq, a = L.frequencies(rotary or dim, theta, scaling, factor, original)
-    return spec, (freq, attention or a, layout)
-
-
-def f64(t):
-    return None if t is None else t.detach().double().cpu().numpy()
 
 
 def inputs(dtype, n, hq, hkv, d, fused, seed, most=5000):
