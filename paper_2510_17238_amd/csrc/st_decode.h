@@ -61,24 +61,24 @@ inline size_t split_lds_bytes(int rows, int d) { return sizeof(float) * size_t(k
 // so and has to reach the row (its weight 2^(-inf) = 0 keeps a NaN one).
 __device__ __forceinline__ bool holds_nothing(float m, float l) { return m == -INFINITY && l == 0.f; }
 
-// log-sum-exp merge of the waves' states into the unit's partial result at row slot `slot`
+// log-sum-exp merge of the waves' states of `rows` rows into the unit's partial result at row slot `slot`
 template <int D>
-__device__ __forceinline__ void merge_waves(const SplitLds<D>& sm, const DecodeArgs& a, int64_t slot) {
-    for (int e = int(threadIdx.x) * 4; e < a.rows * D; e += 64 * kSplitWaves * 4) {
+__device__ __forceinline__ void merge_waves(const SplitLds<D>& sm, int rows, const DecodeArgs& a, int64_t slot) {
+    for (int e = int(threadIdx.x) * 4; e < rows * D; e += 64 * kSplitWaves * 4) {
         const int row = e / D, d0 = e % D;
         float m_all = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w) m_all = fmaxf(m_all, sm.m[w * a.rows + row]);
+        for (int w = 0; w < kSplitWaves; ++w) m_all = fmaxf(m_all, sm.m[w * rows + row]);
         const float m_use = m_all == -INFINITY ? 0.f : m_all;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         float den = 0.f;
 #pragma unroll
         for (int w = 0; w < kSplitWaves; ++w) {
-            const float mw = sm.m[w * a.rows + row], lw = sm.l[w * a.rows + row];
+            const float mw = sm.m[w * rows + row], lw = sm.l[w * rows + row];
             if (holds_nothing(mw, lw)) continue;
             const float wt = __builtin_amdgcn_exp2f(mw - m_use);
             den = fmaf(wt, lw, den);
-            const f32x4 o = *reinterpret_cast<const f32x4*>(sm.o + (w * a.rows + row) * D + d0);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(sm.o + (w * rows + row) * D + d0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] = fmaf(wt, o[i], acc[i]);
         }

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * kSplitWaves, 2) void decode_split32_kernel(Dec
         }
     }
     __syncthreads();
-    merge_waves<D>(sm, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
+    merge_waves<D>(sm, a.rows, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
 }
 // LDS of a workgroup: the loop's part (queries, rotations) and the merge's share the space
 inline size_t split32_lds_bytes(int rows, int q_len, int d) {
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(64 * kSplitWaves, 2) void decode_split16_kernel(Dec
         }
     }
     __syncthreads();
-    merge_waves<D>(sm, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
+    merge_waves<D>(sm, a.rows, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
 }
 // LDS of a workgroup: the rotations and the merge share the space
 inline size_t split16_lds_bytes(int rows, int q_len, int d) {
@@ -890,7 +890,7 @@ __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode_split16_fp8_kernel
         }
     }
     __syncthreads();
-    merge_waves<D>(sm, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
+    merge_waves<D>(sm, a.rows, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
 }
 
 // Merge of a row's partial results (both merge kernels): log-sum-exp in a fixed order, run-to-run identical.  D / 4 lanes take a

@@ -24,8 +24,9 @@ struct Codes {
     uint32_t ks[4];
 };
 
-template <int W, typename T>
-__device__ __forceinline__ void load_words(uint32_t (&dst)[W], const T* p) {
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&dst)[W], const uint8_t* base, uint32_t off) {
+    const uint8_t* p = base + off;
     if constexpr (W == 4) {
         const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 #pragma unroll
@@ -51,26 +52,29 @@ struct Pages4 {
         v_pool = reinterpret_cast<const uint8_t*>(cv.v_pool) + h * (D * 8);
         scales = reinterpret_cast<const uint8_t*>(cv.k_scale) + h * D;
     }
+    // step s of this cache, or of the other one where a wave walks both
     __device__ __forceinline__ void load(int s, int page, const uint8_t* kp, const uint8_t* vp, const uint8_t* sp, int n_kv_heads, Codes<D>& c) const {
-        const int lane = int(threadIdx.x) & 63, n = lane & 15, g = lane >> 4;
+        // (64 dims: two lane groups share a block of 32, half of it each.  A page's address stays scalar, beside an
+        // unsigned 32-bit offset per lane, if the compiler sees the offset where it is used: without the empty statement it hoists its 64-bit form)
+        uint32_t lane = threadIdx.x & 63u;
+        asm volatile("" : "+v"(lane));
+        const uint32_t n = lane & 15u, g = lane >> 4;
+        const uint32_t k_off = D == 128 ? lane * 16u : (g >> 1) * 256u + n * 16u + (g & 1u) * 8u, v_off = lane * uint32_t(D / 8);
+        const uint32_t ks_off = D == 128 ? lane : (g >> 1) * 16u + n, vs_off = uint32_t(D / 2) + g * uint32_t(D / 8);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t id = __builtin_amdgcn_readlane(page, 4 * s + u);
-            const uint8_t* k_of = kp + id * n_kv_heads * (D * 8);
-            const uint8_t* v_of = vp + id * n_kv_heads * (D * 8);
-            const uint8_t* s_of = sp + id * n_kv_heads * D;
-            // (64 dims: two lane groups share a block of 32, half of it each)
-            load_words(c.k[u], k_of + (D == 128 ? lane * 16 : (g >> 1) * 256 + n * 16 + (g & 1) * 8));
-            load_words(c.v[u], v_of + lane * (D / 8));
-            c.ks[u] = s_of[D == 128 ? lane : (g >> 1) * 16 + n];
-            load_words(c.vs[u], s_of + D / 2 + g * (D / 8));
+            const int64_t at = int64_t(__builtin_amdgcn_readlane(page, 4 * s + u)) * n_kv_heads;
+            load_words(c.k[u], kp + at * (D * 8), k_off);
+            load_words(c.v[u], vp + at * (D * 8), v_off);
+            c.ks[u] = (sp + at * D)[ks_off];
+            load_words(c.vs[u], sp + at * D, vs_off);
         }
     }
     __device__ __forceinline__ void load(int s, int n_kv_heads, Codes<D>& c) const { load(s, my_page, k_pool, v_pool, scales, n_kv_heads, c); }
 };
 
-// bytes `i` of a scale word as the fp32 power of two
-__device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_float(((w >> (8 * i)) & 0xffu) << 23); }
+// byte `i` of a scale word where the conversion looks for its exponent (it takes nothing else of the operand)
+__device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_float(i < 3 ? w << (23 - 8 * i) : w >> 1); }
 
 __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float scale, int byte) {
     // (the byte is an immediate of the instruction)
@@ -82,15 +86,33 @@ __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float scale, int byte) 
     }
 }
 
-// Running state of 16 RB query rows, row 16 rb + n in the lanes (n, g), in base-2 exponent units.  The reference exponent of a row is the
-// largest score so far (the weight of the row's largest score is 1, which rounds to itself), the sum takes the weights before they are rounded.
-template <int D, int RB>
+__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
+    bf16x2 r;
+    r[0] = (__bf16)lo;
+    r[1] = (__bf16)hi;
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// Running state of a wave: RB blocks of 16 columns, in base-2 exponent units; column n of block r in the lanes (n, g).
+// Few query rows leave most of the 16 columns of a matrix instruction without a row of their own.  They hold the rows again -- COPIES times 16 / COPIES
+// rows --, and each copy takes the softmax of its share of the step's four pages alone (its weights for the others are 0): the exponentials, which
+// cost four times a multiplication, are not formed twice.  The copies are states of their own and are merged at the end (fold_copies).
+// The reference exponent of a column is its largest score so far: the weight of the largest score is 1, which rounds to itself, and it is the
+// largest weights' rounding that shows in the result.  (Moved only when a score exceeds it by 2^8, the exchange between lanes and the rescale
+// of the accumulator are rare and a step of 64 tokens x 32 rows takes 2 % less time, one of 4 rows the same; the rows' distance from 64 bits
+// is a fifth larger, 2.3e-3 against 1.9e-3 of their norm, 1.7e-3 being the rounding of the result.)  The sum takes the weights before they are
+// rounded.
+template <int D, int RB, int COPIES>
 struct State4 {
     static constexpr int KS = D / 32, DB = D / 16, G = D / 32;
-    bf16x8 qf[RB][KS];
+    static constexpr int ROWS = 16 / COPIES, OWN = 4 / COPIES;             // rows of a block; pages of a step that a column takes
+    static constexpr bool QUERIES_IN_LDS = RB > 1;                         // (one copy for the four waves, in fragment order [RB][KS][64 lanes])
+    static constexpr bool SORT = RB > 1;                                   // (see the second product)
+    bf16x8 q[QUERIES_IN_LDS ? 1 : KS];
+    const bf16x8* s_q;
     f32x4 o[RB][DB];
     float m[RB], l[RB];
-    __device__ __forceinline__ State4() {
+    __device__ __forceinline__ explicit State4(const bf16x8* lds) : s_q(lds) {
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             m[r] = -INFINITY;
@@ -99,47 +121,64 @@ struct State4 {
             for (int db = 0; db < DB; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // largest of the four lanes n, n + 16, n + 32, n + 48 of a row
+    static __device__ __forceinline__ int copy() { return (int(threadIdx.x) & 15) / ROWS; }
+    // largest of the four lanes n, n + 16, n + 32, n + 48 of a column
     static __device__ __forceinline__ float column_max(float x) {
         const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
         const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
         const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
         return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
     }
-    // 64 tokens from token `tok` of a cache of `len` visible tokens, of which this lane's row rb sees [0, limit[rb]) and every row [0, limit_min)
+    // 64 tokens from token `tok` of a cache of `len` visible tokens, of which this lane's column of block r sees [0, limit[r]) and every row
+    // [0, limit_min)
     __device__ __forceinline__ void step(Codes<D>& c, int tok, int len, const int (&limit)[RB], int limit_min, float scale_log2) {
-        const int g = int(threadIdx.x & 63) >> 4;
-        f32x4 s[RB][4];
+        const int lane = int(threadIdx.x) & 63, g = lane >> 4, mine = copy();
+        f32x4 s[RB][4], t[RB][OWN];                                      // scores of page u: register i is slot 4 g + i
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float ks = scale_of(c.ks[u], 0);
+        for (int r = 0; r < RB; ++r)
 #pragma unroll
-            for (int r = 0; r < RB; ++r) s[r][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < 4; ++u) s[r][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < KS; ++j) {
+        for (int j = 0; j < KS; ++j) {
+            bf16x8 qf[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) qf[r] = QUERIES_IN_LDS ? s_q[(r * KS + j) * 64 + lane] : q[j];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
                 u32x4 kf;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) kf[i] = fp4_pair(c.k[u][j], ks, i);
+                for (int i = 0; i < 4; ++i) kf[i] = fp4_pair(c.k[u][j], scale_of(c.ks[u], 0), i);
 #pragma unroll
-                for (int r = 0; r < RB; ++r) s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[r][j], s[r][u], 0, 0, 0);
+                for (int r = 0; r < RB; ++r) s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[r], s[r][u], 0, 0, 0);
             }
         }
-        // register i of page u: token tok + 16 u + 4 g + i
-        const int first = tok + 4 * g;
-        const bool whole = tok + 64 <= limit_min;                        // uniform
-        bf16x8 pb[RB][2];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[r][u % OWN][i] = u < OWN || mine == u / OWN ? s[r][u][i] : t[r][u % OWN][i];
+        const int first = tok + 16 * OWN * mine + 4 * g;                 // token of t[.][0][0]; 16 further on for every other page
+        if (tok + 64 > limit_min) {                                      // uniform: a step that reaches some row's limit
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                int left = limit[r] - first;
+                if constexpr (RB > 1) asm volatile("" : "+v"(left));     // (a branch, not 32 selects in every step)
+#pragma unroll
+                for (int v = 0; v < OWN; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[r][v][i] = 16 * v + i < left ? t[r][v][i] : -INFINITY;
+            }
+        }
+        uint32_t p[RB][OWN][SORT ? 2 : 4];                               // weights as bf16: pairs of slots, or one beside a 0
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             float mx = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int v = 0; v < OWN; ++v)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = s[r][u][i] * scale_log2;
-                    if (!whole) x = first + 16 * u + i < limit[r] ? x : -INFINITY;
-                    s[r][u][i] = x;
-                    mx = fmaxf(mx, x);
-                }
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, t[r][v][i]);
+            mx *= scale_log2;                                            // (which is positive)
             if (__any(mx > m[r])) {
                 const float top = fmaxf(column_max(mx), m[r]);
                 const float alpha = top > -INFINITY ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
@@ -150,14 +189,20 @@ struct State4 {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[r][db][i] *= alpha;
             }
-            const float ref = m[r] > -INFINITY ? m[r] : 0.f;             // (nothing seen so far, or NaN alone)
+            const float ref = m[r] > -INFINITY ? -m[r] : 0.f;            // (nothing seen so far, or NaN alone)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int v = 0; v < OWN; ++v)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(s[r][u][i] - ref);
-                    l[r] += p;
-                    pb[r][u >> 1][4 * (u & 1) + i] = (__bf16)p;
+                for (int i = 0; i < 4; i += 2) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(t[r][v][i], scale_log2, ref)), b = __builtin_amdgcn_exp2f(fmaf(t[r][v][i + 1], scale_log2, ref));
+                    l[r] += a;
+                    l[r] += b;
+                    if constexpr (SORT) {
+                        p[r][v][i / 2] = pair_bf16(a, b);
+                    } else {
+                        p[r][v][i] = pair_bf16(a, 0.f);
+                        p[r][v][i + 1] = pair_bf16(b, 0.f);
+                    }
                 }
         }
         if (tok + 64 > len) {
@@ -166,79 +211,129 @@ struct State4 {
             for (int u = 0; u < 4; ++u) {
                 uint32_t keep = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep |= first + 16 * u + i < len ? 0xffu << (8 * i) : 0u;
+                for (int i = 0; i < 4; ++i) keep |= tok + 16 * u + 4 * g + i < len ? 0xffu << (8 * i) : 0u;
 #pragma unroll
                 for (int gg = 0; gg < G; ++gg) c.vs[u][gg] &= keep;
             }
         }
+        // The second product.  A converted dword is one slot with dims 32 gg + m and 32 gg + 16 + m, two k-values of an operand whose columns are both
+        // sets of dims.  Few rows: the weights go in twice, beside a 0 each, for the lower dims and for the upper ones -- twice the matrix
+        // instructions, for which the pipe has the time.  Two blocks of rows (SORT): the dwords of two slots are sorted into an operand of either
+        // set, one more vector instruction per conversion for half the matrix instructions of both blocks.
+        if constexpr (SORT) {
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
+            for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-            for (int gg = 0; gg < G; ++gg) {
-                // eight tokens (four of page 2 hf, four of the next), dims 32 gg + m and 32 gg + 16 + m
-                uint32_t w[8];
+                for (int gg = 0; gg < G; ++gg) {
+                    u32x4 lo, hi;                                        // four slots of page 2 hf, four of the next
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = fp4_pair(c.v[2 * hf + (e >> 2)][gg], scale_of(c.vs[2 * hf + (e >> 2)][gg], e & 3), e & 3);
-                u32x4 lo, hi;
+                    for (int e = 0; e < 4; ++e) {
+                        const int u = 2 * hf + (e >> 1), i = 2 * (e & 1);
+                        const uint32_t a = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i), i), b = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i + 1), i + 1);
+                        lo[e] = __builtin_amdgcn_perm(b, a, 0x05040100);
+                        hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302);
+                    }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100);
-                    hi[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302);
+                    for (int r = 0; r < RB; ++r) {
+                        const u32x4 w = {p[r][2 * hf][0], p[r][2 * hf][1], p[r][2 * hf + 1][0], p[r][2 * hf + 1][1]};
+                        o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, w), o[r][2 * gg], 0, 0, 0);
+                        o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, w), o[r][2 * gg + 1], 0, 0, 0);
+                    }
                 }
+        } else {
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pb[r][hf], o[r][2 * gg], 0, 0, 0);
-                    o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pb[r][hf], o[r][2 * gg + 1], 0, 0, 0);
+            for (int u = 0; u < 4; ++u) {
+                u32x4 lo[RB], hi[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        lo[r][i] = COPIES == 1 || mine == u / OWN ? p[r][u % OWN][i] : 0u;
+                        hi[r][i] = lo[r][i] << 16;
+                    }
+#pragma unroll
+                for (int gg = 0; gg < G; ++gg) {
+                    u32x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i), i);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo[r]), o[r][2 * gg], 0, 0, 0);
+                        o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi[r]), o[r][2 * gg + 1], 0, 0, 0);
+                    }
                 }
             }
+        }
+    }
+    // The four lanes of a column and the copies of a row merged, in a fixed order; afterwards every lane of a row holds its state.
+    __device__ __forceinline__ void fold_copies() {
+        auto from = [](float x, auto ctrl) {
+            return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+        };
+        using By8 = std::integral_constant<int, 0x128>;                  // row_ror:8, row_ror:4
+        using By4 = std::integral_constant<int, 0x124>;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            l[r] += __shfl_xor(l[r], 16);
+            l[r] += __shfl_xor(l[r], 32);
+            if constexpr (COPIES > 1) {
+                float top = fmaxf(m[r], from(m[r], By8{}));
+                if constexpr (COPIES == 4) top = fmaxf(top, from(top, By4{}));
+                const float alpha = __builtin_amdgcn_exp2f(m[r] - (top > -INFINITY ? top : 0.f));
+                m[r] = top;
+                auto sum = [&](float x) {
+                    x *= alpha;
+                    x += from(x, By8{});
+                    if constexpr (COPIES == 4) x += from(x, By4{});
+                    return x;
+                };
+                l[r] = sum(l[r]);
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[r][db][i] = sum(o[r][db][i]);
+            }
+        }
     }
 };
 
-// The queries of (sequence b, KV head h): row 16 rb + n is token row / G, head row % G; rows past the end repeat the last one (never stored).
-// Fragment j holds dims dim0(g) + 8 j + e.  a.rope: rotated by the row's position, out of the table of the q_len positions.
-template <int D, int RB>
-__device__ __forceinline__ void load_queries(State4<D, RB>& st, const DecodeArgs& a, int b, int h, const float2* s_rot) {
-    constexpr int KS = D / 32;
-    const int lane = int(threadIdx.x) & 63, n = lane & 15, g = lane >> 4, dim0 = (D / 4) * g;
+// Fragment j of the queries of (sequence b, KV head h), block r: row 16 r + n % (16 / COPIES) is token row / G, head row % G (rows past the end repeat
+// the last one, never stored); dims D / 4 g + 8 j + e.  a.rope: rotated by the row's position, out of the table of the q_len positions.
+template <int D, int COPIES>
+__device__ __forceinline__ bf16x8 query_fragment(const DecodeArgs& a, int b, int h, int r, int j, const float2* s_rot) {
+    const int lane = int(threadIdx.x) & 63, n = (lane & 15) % (16 / COPIES), d0 = (D / 4) * (lane >> 4) + 8 * j;
+    const int row = min(16 * r + n, a.rows - 1), t = row / a.group;
+    const uint16_t* qp = a.q + ((int64_t(b) * a.q_len + t) * a.n_q_heads + h * a.group + (row - t * a.group)) * D;
+    bf16x8 x = *reinterpret_cast<const bf16x8*>(qp + d0);
+    if (a.rope) {
+        const bool upper = d0 >= D / 2;
+        const int other0 = upper ? d0 - D / 2 : d0 + D / 2;
+        const bf16x8 y = *reinterpret_cast<const bf16x8*>(qp + other0);
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int row = min(16 * r + n, a.rows - 1), t = row / a.group;
-        const uint16_t* qp = a.q + ((int64_t(b) * a.q_len + t) * a.n_q_heads + h * a.group + (row - t * a.group)) * D;
-        const bool upper = dim0 >= D / 2;
-        const int other0 = upper ? dim0 - D / 2 : dim0 + D / 2;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-            bf16x8 x = *reinterpret_cast<const bf16x8*>(qp + dim0 + 8 * j);
-            if (a.rope) {
-                const bf16x8 y = *reinterpret_cast<const bf16x8*>(qp + other0 + 8 * j);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 cs = s_rot[t * (D / 2) + (upper ? other0 : dim0) + 8 * j + e];
-                    const float own = float(x[e]), part = float(y[e]);
-                    x[e] = (__bf16)(upper ? own * cs.x + part * cs.y : own * cs.x - part * cs.y);
-                }
-            }
-            st.qf[r][j] = x;
+        for (int e = 0; e < 8; ++e) {
+            const float2 cs = s_rot[t * (D / 2) + (upper ? other0 : d0) + e];
+            const float own = float(x[e]), part = float(y[e]);
+            x[e] = (__bf16)(upper ? own * cs.x + part * cs.y : own * cs.x - part * cs.y);
         }
     }
+    return x;
 }
 
 // Row limits of a step over a cache: reasoning token j is seen by query token t where j <= len - q_len + t, the source slice by all
-template <int RB>
+template <int RB, int COPIES>
 __device__ __forceinline__ void row_limits(int (&limit)[RB], const DecodeArgs& a, bool is_src, int len) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        const int t = min(16 * r + (int(threadIdx.x) & 15), a.rows - 1) / a.group;
+        const int t = min(16 * r + (int(threadIdx.x) & 15) % (16 / COPIES), a.rows - 1) / a.group;
         limit[r] = is_src ? len : min(max(len - a.q_len + t + 1, 0), len);
     }
 }
 
-template <int D, int RB>
-__global__ __launch_bounds__(64 * kSplitWaves, 2) void decode4_split_kernel(DecodeArgs a) {
+template <int D, int RB, int COPIES>
+__global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(DecodeArgs a) {
     constexpr int DB = D / 16;
-    // (cos, sin) of the q_len query positions; after the loop: SplitLds
+    // two blocks of rows: query fragments; behind them the (cos, sin) of the q_len query positions; after the loop: SplitLds
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    float2* s_rot = reinterpret_cast<float2*>(smem_raw);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nc = a.ncs + a.ncr;
     const unsigned bh = blockIdx.x / unsigned(nc);       // (sequence, KV head)
@@ -252,48 +347,60 @@ __global__ __launch_bounds__(64 * kSplitWaves, 2) void decode4_split_kernel(Deco
     if (unit0 >= len) return;
     const int n_steps = (min(len - unit0, a.chunk) - 64 * wave + 64 * kSplitWaves - 1) / (64 * kSplitWaves);
     int limit[RB];
-    row_limits<RB>(limit, a, is_src, len);
+    row_limits<RB, COPIES>(limit, a, is_src, len);
     const int limit_min = is_src ? len : min(max(len - a.q_len + 1, 0), len);
-    State4<D, RB> st;
+    using State = State4<D, RB, COPIES>;
+    constexpr int KS = D / 32;
+    bf16x8* s_q = reinterpret_cast<bf16x8*>(smem_raw);
+    float2* s_rot = reinterpret_cast<float2*>(smem_raw + (State::QUERIES_IN_LDS ? RB * KS * 64 * sizeof(bf16x8) : 0));
     if (a.rope) {
         const int len_r = min(max(a.rsn_len[b], 0), a.rsn.max_pages * kPage);
         rope_table_to_lds<D>(s_rot, len_r - a.q_len, a.q_len, rope_frequency<D>(a.freq), 64 * kSplitWaves);
         lds_barrier();
     }
-    load_queries<D, RB>(st, a, b, h, s_rot);
+    State st(s_q);
+    if constexpr (State::QUERIES_IN_LDS) {
+        for (int i = wave; i < RB * KS; i += kSplitWaves) s_q[i * 64 + lane] = query_fragment<D, COPIES>(a, b, h, i / KS, i % KS, s_rot);
+        lds_barrier();
+    } else {
+#pragma unroll
+        for (int j = 0; j < KS; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, s_rot);
+    }
+    const int tok0 = unit0 + 64 * wave;
     for (int s = 0; s < n_steps; ++s) {
         Codes<D> codes;
         pages.load(s, a.n_kv_heads, codes);
-        st.step(codes, unit0 + 64 * (wave + kSplitWaves * s), len, limit, limit_min, a.scale_log2);
+        st.step(codes, tok0 + 64 * kSplitWaves * s, len, limit, limit_min, a.scale_log2);
     }
-    __syncthreads();                                    // everybody is done with the rotations
-    const SplitLds<D> sm(smem_raw, a.rows);
+    st.fold_copies();
+    // the waves' states meet in LDS, a block of rows at a time: with both at once (66 KB) a compute unit would hold two workgroups, not three
     const int n = lane & 15, g = lane >> 4;
+    const int64_t slot = ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows;
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        float l = st.l[r] + __shfl_xor(st.l[r], 16);
-        l += __shfl_xor(l, 32);
-        const int row = 16 * r + n;
-        if (row < a.rows) {
+        __syncthreads();                                // everybody is done with the queries and rotations, with the block before
+        const int rows = min(a.rows - 16 * r, 16);
+        const SplitLds<D> sm(smem_raw, rows);
+        if (n < 16 / COPIES && n < rows) {
             // lane (n, g), block db, register i  <->  d = 16 db + 4 g + i
-            float* po = sm.o + (wave * a.rows + row) * D;
+            float* po = sm.o + (wave * rows + n) * D;
 #pragma unroll
             for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[r][db];
             if (g == 0) {
-                sm.m[wave * a.rows + row] = st.m[r];
-                sm.l[wave * a.rows + row] = l;
+                sm.m[wave * rows + n] = st.m[r];
+                sm.l[wave * rows + n] = st.l[r];
             }
         }
+        __syncthreads();
+        merge_waves<D>(sm, rows, a, slot + 16 * r);
     }
-    __syncthreads();
-    merge_waves<D>(sm, a, ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows);
 }
 
 // Short caches: a workgroup of eight waves takes all of a (sequence, KV head) and finishes its rows -- one launch, no partial results.  Steps are
 // dealt out as in the bf16 kernel: reasoning steps from the first wave up, source steps from the last one down.
 constexpr int kSmallWaves4 = 8;
 
-template <int D>
+template <int D, int COPIES>
 __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(DecodeArgs a, uint16_t* __restrict__ out, float* __restrict__ lse) {
     constexpr int DB = D / 16, W = kSmallWaves4;
     extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -306,15 +413,16 @@ __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(Dec
     const int len_s = min(max(a.src_len[b], 0), a.src.max_pages * kPage), len_r = min(max(a.rsn_len[b], 0), a.rsn.max_pages * kPage);
     const int steps_s = (len_s - 64 * (W - 1 - wave) + 64 * W - 1) / (64 * W), steps_r = (len_r - 64 * wave + 64 * W - 1) / (64 * W);
     int limit_s[1], limit_r[1];
-    row_limits<1>(limit_s, a, true, len_s);
-    row_limits<1>(limit_r, a, false, len_r);
+    row_limits<1, COPIES>(limit_s, a, true, len_s);
+    row_limits<1, COPIES>(limit_r, a, false, len_r);
     const int limit_min = min(max(len_r - a.q_len + 1, 0), len_r);
-    State4<D, 1> st;
+    State4<D, 1, COPIES> st(nullptr);
     if (a.rope) {
         rope_table_to_lds<D>(sm_rot, len_r - a.q_len, a.q_len, rope_frequency<D>(a.freq), 64 * W);
         lds_barrier();
     }
-    load_queries<D, 1>(st, a, b, h, sm_rot);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, sm_rot);
     for (int x = 0; x < steps_r + steps_s; ++x) {
         const bool r = x < steps_r;
         const int s = r ? x : x - steps_r;
@@ -324,14 +432,13 @@ __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(Dec
         const int limit[1] = {r ? limit_r[0] : limit_s[0]};
         st.step(codes, 64 * ((r ? wave : W - 1 - wave) + W * s), r ? len_r : len_s, limit, r ? limit_min : len_s, a.scale_log2);
     }
-    float l = st.l[0] + __shfl_xor(st.l[0], 16);
-    l += __shfl_xor(l, 32);
+    st.fold_copies();
     const int n = lane & 15, g = lane >> 4;
-    if (n < a.rows) {
+    if (n < 16 / COPIES && n < a.rows) {
         float* po = sm_o + (wave * a.rows + n) * D;
 #pragma unroll
         for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[0][db];
-        if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], l};
+        if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], st.l[0]};
     }
     __syncthreads();
     merge_and_store<D, W, W>(sm_o, sm_ml, a, b, h, out, lse);
@@ -345,14 +452,17 @@ static st_status allow_lds(Kernel kernel, size_t bytes) {
 }
 
 st_status launch_decode4(const DecodeArgs& a, int head_dim, int64_t units, hipStream_t s) {
-    const size_t rot = size_t(a.q_len) * (head_dim / 2) * sizeof(float2), smem = std::max(rot, split_lds_bytes(a.rows, head_dim));
+    const size_t loop = (a.rows > 16 ? size_t(2) * (head_dim / 32) * 64 * 16 : 0) + size_t(a.q_len) * (head_dim / 2) * sizeof(float2);
+    const size_t smem = std::max(loop, split_lds_bytes(std::min(a.rows, 16), head_dim));
     auto go = [&](auto kernel) -> st_status {
         const st_status r = allow_lds(kernel, smem);
         if (r == ST_OK) hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(64 * kSplitWaves), smem, s, a);
         return r;
     };
-    if (a.rows <= 16) return head_dim == 64 ? go(decode4_split_kernel<64, 1>) : go(decode4_split_kernel<128, 1>);
-    return head_dim == 64 ? go(decode4_split_kernel<64, 2>) : go(decode4_split_kernel<128, 2>);
+    if (a.rows <= 4) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 4>) : go(decode4_split_kernel<128, 1, 4>);
+    if (a.rows <= 8) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 2>) : go(decode4_split_kernel<128, 1, 2>);
+    if (a.rows <= 16) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 1>) : go(decode4_split_kernel<128, 1, 1>);
+    return head_dim == 64 ? go(decode4_split_kernel<64, 2, 1>) : go(decode4_split_kernel<128, 2, 1>);
 }
 
 st_status launch_decode4_small(const DecodeArgs& a, int head_dim, uint16_t* out, float* lse, hipStream_t s) {
@@ -362,7 +472,9 @@ st_status launch_decode4_small(const DecodeArgs& a, int head_dim, uint16_t* out,
         if (r == ST_OK) hipLaunchKernelGGL(kernel, dim3((unsigned)(a.batch * a.n_kv_heads)), dim3(64 * kSmallWaves4), smem, s, a, out, lse);
         return r;
     };
-    return head_dim == 64 ? go(decode4_small_kernel<64>) : go(decode4_small_kernel<128>);
+    if (a.rows <= 4) return head_dim == 64 ? go(decode4_small_kernel<64, 4>) : go(decode4_small_kernel<128, 4>);
+    if (a.rows <= 8) return head_dim == 64 ? go(decode4_small_kernel<64, 2>) : go(decode4_small_kernel<128, 2>);
+    return head_dim == 64 ? go(decode4_small_kernel<64, 1>) : go(decode4_small_kernel<128, 1>);
 }
 
 }  // namespace st
