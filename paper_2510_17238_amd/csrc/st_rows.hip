@@ -8,8 +8,10 @@
 //
 // Keys are normalised and rotated in 64 bits and rounded to bf16 once; codes are formed from those bf16 rows.  64 bits, because a code is
 // as wide as a sixth of its block's largest value: 32 bits would put a few keys of every million on the other side of the line between two codes,
-// and the same row would not always be stored alike.  fp64 runs at the rate of unpacked fp32 here, so it costs registers, not time.
+// and the same row would not always be stored alike.  Nearly every row's codes are the same at both ends of the interval that 32-bit arithmetic
+// leaves, though, and those rows are done with it (quick_key).
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -32,10 +34,11 @@ struct RowsArgs {
     double eps;
     int rotate, write_len;       // write_len: the workgroup of a sequence's first page writes the new length
     RopeTable rope;
+    double2 step[64];            // (cos, sin) of the pairs' angles per token
 };
 
 // 64 bits rounded to bf16 in ONE rounding: to 32 bits with the last bit set if anything was lost, then to nearest even
-__device__ __forceinline__ uint16_t f64_to_bf16_bits(double x) {
+__device__ __forceinline__ uint32_t f64_to_bf16_bits(double x) {
     const float f = float(x);
     uint32_t u = __float_as_uint(f);
     if (double(f) != x) {
@@ -43,6 +46,37 @@ __device__ __forceinline__ uint16_t f64_to_bf16_bits(double x) {
         u |= 1u;
     }
     return f32_to_bf16_bits(__uint_as_float(u));
+}
+// Eight at once.  By way of 32 bits, rounded to nearest, the result is the same unless the 32-bit value lies exactly between two bf16 values (its
+// lower half is 0x8000): a lane that has such a value, one in some thousands, takes the long way with all of them.
+__device__ __forceinline__ u32x4 f64x8_to_bf16(const double (&x)[8]) {
+    uint32_t f[8];
+    u32x4 out;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 between = {0xffffu, 0xffffu};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __float_as_uint(float(x[i]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bf16x2 r;
+        r[0] = (__bf16)__uint_as_float(f[2 * i]);
+        r[1] = (__bf16)__uint_as_float(f[2 * i + 1]);
+        out[i] = __builtin_bit_cast(uint32_t, r);
+        const uint32_t lower = __builtin_amdgcn_perm(f[2 * i + 1], f[2 * i], 0x05040100) ^ 0x80008000u;
+        between = __builtin_elementwise_min(between, __builtin_bit_cast(u16x2, lower));
+    }
+    if (between[0] == 0 || between[1] == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = f64_to_bf16_bits(x[2 * i]) | (f64_to_bf16_bits(x[2 * i + 1]) << 16);
+    return out;
+}
+// x^(-1/2) in 64 bits: the instruction's estimate and Newton's iteration (each squares the error)
+__device__ __forceinline__ double inverse_root(double x) {
+    double y = __builtin_amdgcn_rsq(x);
+    const double h = 0.5 * x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = fma(y, fma(-h * y, y, 0.5), y);
+    return y;
 }
 
 constexpr int kScaleExpLeast = -100;             // of 8-bit rows and 4-bit blocks alike
@@ -66,17 +100,19 @@ __device__ __forceinline__ int scale_exponent(uint32_t top, int m128, int e) {
     return max(int(top >> 7) - 127 - e + (int(top & 127u) > m128 ? 1 : 0), kScaleExpLeast);
 }
 
-// Storage formats.  A lane stores its eight key dims (8 c ..) of slot s, a thread of a whole page's image its share of V.
-//   PIECE bytes a lane holds of a row; v_at(slot, d) byte of value element in a page of one head
+// Storage formats.  encode: a lane's eight values (bf16, of dims 8 c ..) as the format's codes, with the scale's exponent; put_*: to the token's place
+// in a page of one head.  PIECE: bytes of the eight.
 template <int FMT, int D>
 struct Store;
 
 template <int D>
 struct Store<ST_BF16, D> {
     static constexpr int PIECE = 16;
-    static __device__ __forceinline__ u32x4 code(const u32x4& x, bool, const CacheView&, int64_t, int, int) { return x; }
-    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const u32x4& p) { *reinterpret_cast<u32x4*>(page + (c * kPage + slot) * 16) = p; }
-    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const u32x4& p) {
+    using Code = u32x4;
+    static __device__ __forceinline__ Code encode(const u32x4& x) { return x; }
+    static __device__ __forceinline__ void put_scale(const CacheView&, int64_t, int, int, bool, const Code&) {}
+    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const Code& p) { *reinterpret_cast<u32x4*>(page + (c * kPage + slot) * 16) = p; }
+    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const Code& p) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) *reinterpret_cast<uint16_t*>(page + ((8 * c + e) * kPage + slot) * 2) = uint16_t(p[e / 2] >> (16 * (e & 1)));
     }
@@ -85,27 +121,38 @@ struct Store<ST_BF16, D> {
 template <int D>
 struct Store<ST_FP8_E4M3, D> {
     static constexpr int PIECE = 8;
-    // codes of a lane's eight dims, the row's scale written by the row's first lane
-    static __device__ __forceinline__ u32x4 code(const u32x4& x, bool value, const CacheView& cv, int64_t page_head, int slot, int c) {
+    struct Code {
+        uint32_t w[2];
+        int k;
+    };
+    static __device__ __forceinline__ bool same(const Code& a, const Code& b) { return a.w[0] == b.w[0] && a.w[1] == b.w[1] && a.k == b.k; }
+    static __device__ __forceinline__ Code encode(const u32x4& x) {
         const uint32_t top = row_top<D / 8>(x);
+        Code r;
         // (448 = 1.75 * 2^8.  A row with an infinite or undefined element: that element's code is NaN, the scale the largest there is)
-        const int k = scale_exponent(min(top, 0x7f7fu), 96, 8);
-        if (c == 0) (value ? cv.v_scale : cv.k_scale)[page_head * kPage + slot] = ldexpf(1.f, k);
-        uint32_t w[2] = {0u, 0u};
+        r.k = scale_exponent(min(top, 0x7f7fu), 96, 8);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = ldexpf(__uint_as_float(x[i] << 16), -k), hi = ldexpf(__uint_as_float(x[i] & 0xffff0000u), -k);
-            if (i & 1) w[i / 2] = __builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, w[i / 2], true);
-            else w[i / 2] = __builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, w[i / 2], false);
+        for (int u = 0; u < 2; ++u) {
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f[2 * i] = ldexpf(__uint_as_float(x[2 * u + i] << 16), -r.k);
+                f[2 * i + 1] = ldexpf(__uint_as_float(x[2 * u + i] & 0xffff0000u), -r.k);
+            }
+            r.w[u] = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0u, false);
+            r.w[u] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], r.w[u], true);
         }
-        return u32x4{w[0], w[1], 0u, 0u};
+        return r;
     }
-    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const u32x4& p) {
-        *reinterpret_cast<u32x2*>(page + ((c >> 1) * kPage + slot) * 16 + 8 * (c & 1)) = u32x2{p[0], p[1]};
+    static __device__ __forceinline__ void put_scale(const CacheView& cv, int64_t page_head, int slot, int c, bool value, const Code& p) {
+        if (c == 0) (value ? cv.v_scale : cv.k_scale)[page_head * kPage + slot] = ldexpf(1.f, p.k);
     }
-    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const u32x4& p) {
+    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const Code& p) {
+        *reinterpret_cast<u32x2*>(page + ((c >> 1) * kPage + slot) * 16 + 8 * (c & 1)) = u32x2{p.w[0], p.w[1]};
+    }
+    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const Code& p) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) page[(8 * c + e) * kPage + slot] = uint8_t(p[e / 4] >> (8 * (e & 3)));
+        for (int e = 0; e < 8; ++e) page[(8 * c + e) * kPage + slot] = uint8_t(p.w[e / 4] >> (8 * (e & 3)));
     }
 };
 
@@ -114,44 +161,59 @@ struct Store<ST_FP8_E4M3, D> {
 template <int D>
 struct Store<ST_MXFP4, D> {
     static constexpr int PIECE = 4;
-    static __device__ __forceinline__ u32x4 code(const u32x4& x, bool value, const CacheView& cv, int64_t page_head, int slot, int c) {
+    struct Code {
+        uint32_t w, scale;       // scale: the E8M0 byte
+    };
+    static __device__ __forceinline__ bool same(const Code& a, const Code& b) { return a.w == b.w && a.scale == b.scale; }
+    static __device__ __forceinline__ Code encode(const u32x4& x) {
         const uint32_t top = row_top<4>(x);                  // a block of 32 dims: four lanes
         const bool bad = top >= 0x7f80u;
-        const int k = bad ? 0 : scale_exponent(top, 64, 2);  // 6 = 1.5 * 2^2
-        if ((c & 3) == 0) {
-            uint8_t* scales = reinterpret_cast<uint8_t*>(cv.k_scale) + page_head * D;
-            const int at = value ? D / 2 + ((slot >> 2) * (D / 32) + (c >> 2)) * 4 + (slot & 3) : (c >> 2) * kPage + slot;
-            scales[at] = bad ? uint8_t(255) : uint8_t(k + 127);
-        }
-        const float scale = __uint_as_float(uint32_t(k + 127) << 23);
+        const uint32_t biased = uint32_t(bad ? 127 : scale_exponent(top, 64, 2) + 127);          // 6 = 1.5 * 2^2
+        const float scale = __uint_as_float(biased << 23);
         uint32_t w = 0;
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), scale, 0);
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u), scale, 1);
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x[2] << 16), __uint_as_float(x[2] & 0xffff0000u), scale, 2);
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x[3] << 16), __uint_as_float(x[3] & 0xffff0000u), scale, 3);
-        return u32x4{bad ? 0u : w, 0u, 0u, 0u};
+        return Code{bad ? 0u : w, bad ? 255u : biased};
     }
-    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const u32x4& p) {
-        *reinterpret_cast<uint32_t*>(page + ((c >> 2) * kPage + slot) * 16 + 4 * (c & 3)) = p[0];
+    static __device__ __forceinline__ void put_scale(const CacheView& cv, int64_t page_head, int slot, int c, bool value, const Code& p) {
+        if ((c & 3) != 0) return;
+        uint8_t* scales = reinterpret_cast<uint8_t*>(cv.k_scale) + page_head * D;
+        scales[value ? D / 2 + ((slot >> 2) * (D / 32) + (c >> 2)) * 4 + (slot & 3) : (c >> 2) * kPage + slot] = uint8_t(p.scale);
     }
-    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const u32x4& p) {
-        const uint32_t mine = p[0], other = uint32_t(__builtin_amdgcn_update_dpp(0, int(mine), 0x4e, 0xf, 0xf, true));      // lane c ^ 2
+    static __device__ __forceinline__ void put_key(uint8_t* page, int slot, int c, const Code& p) {
+        *reinterpret_cast<uint32_t*>(page + ((c >> 2) * kPage + slot) * 16 + 4 * (c & 3)) = p.w;
+    }
+    static __device__ __forceinline__ void put_value(uint8_t* page, int slot, int c, const Code& p) {
+        const uint32_t mine = p.w, other = uint32_t(__builtin_amdgcn_update_dpp(0, int(mine), 0x4e, 0xf, 0xf, true));       // lane c ^ 2
         const bool high = (c & 2) != 0;                     // this lane holds the dims 16 further on
-        const uint32_t lo = high ? other : mine, hi = high ? mine : other;
+        // this lane's four of the eight: dims 8 (c % 2) + first .. + 3 within sixteen; their codes as the nibbles of 16 bits
         const int first = high ? 4 : 0;
+        const uint32_t lo = ((high ? other : mine) >> (4 * first)) & 0xffffu, hi = ((high ? mine : other) >> (4 * first)) & 0xffffu;
+        uint8_t* dst = page + ((slot >> 2) * 16 + 8 * (c & 1) + first) * (D / 8) + (c >> 2) * 4 + (slot & 3);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = first + i, m = 8 * (c & 1) + e;   // dim within sixteen
-            page[((slot >> 2) * 16 + m) * (D / 8) + (c >> 2) * 4 + (slot & 3)] = uint8_t(((lo >> (4 * e)) & 15u) | (((hi >> (4 * e)) & 15u) << 4));
-        }
+        for (int i = 0; i < 4; ++i) dst[i * (D / 8)] = uint8_t(((lo >> (4 * i)) & 15u) | (((hi >> (4 * i)) & 15u) << 4));
     }
 };
 
-// A key row's eight dims in a lane, normalised and rotated in 64 bits
+// The lane's place in a rotation, as in the normalising kernels
+struct KeyTurn {
+    int partner, at;             // the lane that holds the partners of its dims; the first of its pairs
+    bool turned, high;           // any of its dims are rotated; they are the second halves of their pairs
+    __device__ __forceinline__ KeyTurn(const RopeTable& rope, int c) {
+        const int half = rope.rot / 2;
+        high = 8 * c >= half;
+        turned = 8 * c < rope.rot;
+        partner = (int(threadIdx.x) & 63) + (turned ? (high ? -half / 8 : half / 8) : 0);
+        at = rope.interleaved ? 4 * c : high ? 8 * c - half : 8 * c;
+    }
+};
+
+// A key row's eight dims in a lane, normalised and rotated in 64 bits; angles: (cos, sin) times a of the token's pairs
 template <int D>
-__device__ __forceinline__ u32x4 transform_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const double2* table) {
+__device__ __forceinline__ u32x4 exact_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const double2* angles) {
     constexpr int L = D / 8;
-    const int c = int(threadIdx.x) % L, half = a.rope.rot / 2;
     double x[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -162,7 +224,7 @@ __device__ __forceinline__ u32x4 transform_key(const u32x4& raw, const RowsArgs&
         double ss = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss = fma(x[i], x[i], ss);
-        const double r = 1.0 / sqrt(row_sum<L>(ss) * (1.0 / D) + a.eps);
+        const double r = inverse_root(fma(row_sum<L>(ss), 1.0 / D, a.eps));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] *= r * double(__uint_as_float(w_raw[i] << 16));
@@ -170,34 +232,102 @@ __device__ __forceinline__ u32x4 transform_key(const u32x4& raw, const RowsArgs&
         }
     }
     if (a.rotate) {
-        const bool turned = 8 * c < a.rope.rot;
+        const KeyTurn turn(a.rope, int(threadIdx.x) % L);
         if (a.rope.interleaved) {
-            if (turned) {
+            if (turn.turned) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const double2 r = table[4 * c + i];
+                    const double2 r = angles[turn.at + i];
                     const double lo = x[2 * i], hi = x[2 * i + 1];
                     x[2 * i] = lo * r.x - hi * r.y;
                     x[2 * i + 1] = hi * r.x + lo * r.y;
                 }
             }
         } else {
-            const bool high = 8 * c >= half;
-            const int partner = (int(threadIdx.x) & 63) + (turned ? (high ? -half / 8 : half / 8) : 0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double other = __shfl(x[i], partner);
-                if (turned) {
-                    const double2 r = table[(high ? 8 * c - half : 8 * c) + i];
-                    x[i] = x[i] * r.x + other * (high ? r.y : -r.y);
+                const double other = __shfl(x[i], turn.partner);
+                if (turn.turned) {
+                    const double2 r = angles[turn.at + i];
+                    x[i] = x[i] * r.x + other * (turn.high ? r.y : -r.y);
                 }
             }
         }
     }
-    u32x4 out;
+    return f64x8_to_bf16(x);
+}
+
+// The same in 32 bits: bf16 rows (lo, hi) between which the row in 64 bits lies, value by value; false if the row's size is not of 32 bits.
+// Roundings, in units of u = 2^-24: the sum of squares 12 and eps, the mean's root half of these and 2 of its own, two products: 11 on a normalised
+// value; cos and sin 1, their products and the sum 2 of |n_i| + |n_j|: 14 a (|n_i| + |n_j|), taken as 20.
+template <int D>
+__device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const float* cos, const float* sin, u32x4& lo, u32x4& hi) {
+    constexpr int L = D / 8;
+    constexpr float kUnits = 20.f / 16777216.f;
+    float x[8], err[8];
+    bool sure = true;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = uint32_t(f64_to_bf16_bits(x[2 * i])) | (uint32_t(f64_to_bf16_bits(x[2 * i + 1])) << 16);
-    return out;
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(raw[i] << 16);
+        x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+    }
+    if (a.k_weight) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+        const float mean = fmaf(row_sum<L>(ss), 1.f / D, float(a.eps));
+        sure = mean > 0x1p-80f && mean < 0x1p80f;
+        const float r = rsqrtf(mean);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = x[2 * i] * r * __uint_as_float(w_raw[i] << 16);
+            x[2 * i + 1] = x[2 * i + 1] * r * __uint_as_float(w_raw[i] & 0xffff0000u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) err[i] = kUnits * fabsf(x[i]);
+    if (a.rotate) {
+        const KeyTurn turn(a.rope, int(threadIdx.x) % L);
+        const float unit = kUnits * float(a.rope.a);
+        if (a.rope.interleaved) {
+            if (turn.turned) {
+                const f32x4 c = *reinterpret_cast<const f32x4*>(cos + turn.at), s = *reinterpret_cast<const f32x4*>(sin + turn.at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = x[2 * i], q = x[2 * i + 1];
+                    err[2 * i] = err[2 * i + 1] = unit * (fabsf(p) + fabsf(q));
+                    x[2 * i] = fmaf(p, c[i], -(q * s[i]));
+                    x[2 * i + 1] = fmaf(q, c[i], p * s[i]);
+                }
+            }
+        } else {
+            float other[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], turn.partner);
+            if (turn.turned) {
+                const float sign = turn.high ? 1.f : -1.f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const f32x4 c = *reinterpret_cast<const f32x4*>(cos + turn.at + 4 * u), s = *reinterpret_cast<const f32x4*>(sin + turn.at + 4 * u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 4 * u + i;
+                        err[e] = unit * (fabsf(x[e]) + fabsf(other[e]));
+                        x[e] = fmaf(x[e], c[i], other[e] * (sign * s[i]));
+                    }
+                }
+            }
+        }
+    }
+    bf16x8 l, h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        l[i] = (__bf16)(x[i] - err[i]);
+        h[i] = (__bf16)(x[i] + err[i]);
+    }
+    lo = __builtin_bit_cast(u32x4, l);
+    hi = __builtin_bit_cast(u32x4, h);
+    return sure;
 }
 
 constexpr int kRowsThreads = 256;
@@ -208,10 +338,24 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
     constexpr int L = D / 8, RP = kRowsThreads / L, HEADS = RP / kPage;      // rows, whole pages of a head per pass
     constexpr int IMAGE = D * kPage * S::PIECE / 8;                          // bytes of a page of one head
     extern __shared__ __align__(16) unsigned char smem[];
-    double2* table = reinterpret_cast<double2*>(smem);                       // [16][rot / 2] (cos, sin) times a
-    uint8_t* image = smem + (a.rotate ? kPage * (a.rope.rot / 2) * sizeof(double2) : 0);         // [2][HEADS][IMAGE]
+    constexpr bool CODED = FMT != ST_BF16;
+    // (cos, sin) times a of sixteen tokens, [16][rot / 2]; the same in 32 bits, each for itself (not for bf16 rows, which are all formed in 64 bits)
+    const int half = a.rope.rot / 2, angles = a.rotate ? kPage * half : 0;
+    double2* table = reinterpret_cast<double2*>(smem);
+    float *s_cos = reinterpret_cast<float*>(table + angles), *s_sin = s_cos + angles;
+    uint8_t* image = reinterpret_cast<uint8_t*>(CODED ? s_sin + angles : s_cos);                 // [2][HEADS][IMAGE]
     const int group = int(blockIdx.x) % a.head_groups, pi = (int(blockIdx.x) / a.head_groups) % a.touched, b = int(blockIdx.x) / (a.head_groups * a.touched);
     const int capacity = a.cache.max_pages * kPage;
+    const int h0 = group * a.heads, n_heads = min(a.heads, a.cache.n_kv_heads - h0);
+    const int c = int(threadIdx.x) % L, row = int(threadIdx.x) / L;
+    // one token per sequence: its rows do not depend on the lengths, and are asked for before them
+    u32x4 k_next = {0u, 0u, 0u, 0u}, v_next = {0u, 0u, 0u, 0u};
+    if (a.max_new == 1 && row < n_heads) {
+        k_next = *reinterpret_cast<const u32x4*>(a.k_new + b * a.k_stride + (h0 + row) * D + 8 * c);
+        v_next = *reinterpret_cast<const u32x4*>(a.v_new + b * a.v_stride + (h0 + row) * D + 8 * c);
+    }
+    u32x4 w_raw = {0u, 0u, 0u, 0u};
+    if (a.k_weight) w_raw = *reinterpret_cast<const u32x4*>(a.k_weight + 8 * c);
     const int start = min(max(a.start_len ? a.start_len[b] : a.cache.appended_len[b], 0), capacity);
     int n = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
     n = min(n, capacity - start);                                            // tokens past the page table are dropped
@@ -226,48 +370,81 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
     const int id = a.cache.page_table[int64_t(b) * a.cache.max_pages + page];
     if (id < 0 || id >= a.cache.n_pages) return;                             // never write outside the pool
     const int slot_lo = lo - page * kPage, cnt = hi - lo;
-    const int h0 = group * a.heads, n_heads = min(a.heads, a.cache.n_kv_heads - h0);
-    const int c = int(threadIdx.x) % L, row = int(threadIdx.x) / L;
     const int64_t tok0 = int64_t(b) * a.max_new + (lo - start);
-
-    u32x4 w_raw = {0u, 0u, 0u, 0u};
-    if (a.k_weight) w_raw = *reinterpret_cast<const u32x4*>(a.k_weight + 8 * c);
-    const int half = a.rope.rot / 2;
     if (a.rotate) {
-        for (int w = int(threadIdx.x); w < cnt * half; w += kRowsThreads) {
-            const int t = w / half, i = w - t * half;
-            const double rev = double(lo + t) * a.rope.f[i] * 0.15915494309189535;       // angle / 2 pi; a token's index is its position id
-            double sn, cs;
-            sincospi(2.0 * (rev - rint(rev)), &sn, &cs);
-            table[w] = double2{cs * a.rope.a, sn * a.rope.a};
+        // four consecutive tokens of a pair per thread: one evaluation at the first (a token's index is its position id), then turned on by the pair's
+        // angle per token
+        for (int w = int(threadIdx.x); w < (cnt + 3) / 4 * half; w += kRowsThreads) {
+            const int t0 = w / half, i = w - t0 * half;
+            const double rev = double(lo + 4 * t0) * a.rope.f[i] * 0.15915494309189535;          // angle / 2 pi
+            const double2 step = a.step[i];
+            double2 r;
+            sincospi(2.0 * (rev - rint(rev)), &r.y, &r.x);
+            r.x *= a.rope.a;
+            r.y *= a.rope.a;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                table[(4 * t0 + t) * half + i] = r;                  // (the table holds sixteen tokens)
+                if constexpr (CODED) {
+                    s_cos[(4 * t0 + t) * half + i] = float(r.x);
+                    s_sin[(4 * t0 + t) * half + i] = float(r.y);
+                }
+                r = double2{r.x * step.x - r.y * step.y, r.y * step.x + r.x * step.y};
+            }
         }
         __syncthreads();
     }
     auto load = [&](const uint16_t* src, int64_t stride, int t, int h) { return *reinterpret_cast<const u32x4*>(src + (tok0 + t) * stride + (h0 + h) * D + 8 * c); };
     auto page_of = [&](uint16_t* pool, int h) { return reinterpret_cast<uint8_t*>(pool) + (int64_t(id) * a.cache.n_kv_heads + h0 + h) * IMAGE; };
-    auto key = [&](const u32x4& raw, int t) { return a.k_weight || a.rotate ? transform_key<D>(raw, a, w_raw, table + t * half) : raw; };
+    auto key = [&](const u32x4& raw, int t) -> typename S::Code {
+        if (!a.k_weight && !a.rotate) return S::encode(raw);
+        if constexpr (CODED) {
+            u32x4 x_lo, x_hi;
+            const bool sure = quick_key<D>(raw, a, w_raw, s_cos + t * half, s_sin + t * half, x_lo, x_hi);
+            const typename S::Code c_lo = S::encode(x_lo), c_hi = S::encode(x_hi);
+            if (!__any(!sure || !S::same(c_lo, c_hi))) return c_lo;          // (else one wave in some tens)
+        }
+        return S::encode(exact_key<D>(raw, a, w_raw, table + t * half));
+    };
+    auto put = [&](const typename S::Code& code, bool value, uint8_t* page, int64_t page_head, int slot) {
+        S::put_scale(a.cache, page_head, slot, c, value, code);
+        if (value) S::put_value(page, slot, c, code);
+        else S::put_key(page, slot, c, code);
+    };
 
     if (cnt < kPage) {
         // part of a page: rows (head, token) in turn, straight to their places
         for (int r = row; r < cnt * n_heads; r += RP) {
             const int h = r / cnt, t = r - h * cnt;
-            const u32x4 k_raw = load(a.k_new, a.k_stride, t, h), v_raw = load(a.v_new, a.v_stride, t, h);
+            if (a.max_new > 1 || r >= RP) {
+                k_next = load(a.k_new, a.k_stride, t, h);
+                v_next = load(a.v_new, a.v_stride, t, h);
+            }
+            const u32x4 k_raw = k_next, v_raw = v_next;
             const int64_t page_head = int64_t(id) * a.cache.n_kv_heads + h0 + h;
-            S::put_key(page_of(a.cache.k_pool, h), slot_lo + t, c, S::code(key(k_raw, t), false, a.cache, page_head, slot_lo + t, c));
-            S::put_value(page_of(a.cache.v_pool, h), slot_lo + t, c, S::code(v_raw, true, a.cache, page_head, slot_lo + t, c));
+            put(key(k_raw, t), false, page_of(a.cache.k_pool, h), page_head, slot_lo + t);
+            put(S::encode(v_raw), true, page_of(a.cache.v_pool, h), page_head, slot_lo + t);
         }
         return;
     }
     // a whole page: HEADS heads per pass, values through an image of their pages in LDS (two images in turn: one barrier per pass)
     const int t = row % kPage, sub = row / kPage;
+    if (sub < n_heads) {
+        k_next = load(a.k_new, a.k_stride, t, sub);
+        v_next = load(a.v_new, a.v_stride, t, sub);
+    }
     for (int h = 0, turn = 0; h < n_heads; h += HEADS, turn ^= 1) {
         uint8_t* img = image + turn * (HEADS * IMAGE);
         const int mine = h + sub;
         if (mine < n_heads) {
-            const u32x4 k_raw = load(a.k_new, a.k_stride, t, mine), v_raw = load(a.v_new, a.v_stride, t, mine);
+            const u32x4 k_raw = k_next, v_raw = v_next;
+            if (mine + HEADS < n_heads) {
+                k_next = load(a.k_new, a.k_stride, t, mine + HEADS);
+                v_next = load(a.v_new, a.v_stride, t, mine + HEADS);
+            }
             const int64_t page_head = int64_t(id) * a.cache.n_kv_heads + h0 + mine;
-            S::put_value(img + sub * IMAGE, t, c, S::code(v_raw, true, a.cache, page_head, t, c));
-            S::put_key(page_of(a.cache.k_pool, mine), t, c, S::code(key(k_raw, t), false, a.cache, page_head, t, c));
+            put(S::encode(v_raw), true, img + sub * IMAGE, page_head, t);
+            put(key(k_raw, t), false, page_of(a.cache.k_pool, mine), page_head, t);
         }
         __syncthreads();
         // (heads of a page lie one behind the other: the image is one run of bytes)
@@ -290,6 +467,8 @@ __global__ void append_rows_len_kernel(int32_t* __restrict__ appended_len, const
     appended_len[b] = start + min(n, capacity - start);
 }
 
+constexpr int kAppendWorkgroups = 2048;
+
 st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
                       const int32_t* start_len, const int32_t* n_new, int max_new, int batch, const void* k_weight, double eps,
                       const RopeTable* rope, hipStream_t s) {
@@ -306,11 +485,21 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     a.k_weight = static_cast<const uint16_t*>(k_weight);
     a.eps = eps;
     a.rotate = rope != nullptr;
-    if (rope) a.rope = *rope;
+    if (rope) {
+        a.rope = *rope;
+        // (128 calls of cos and sin: kept as the table itself is)
+        static thread_local double kept_f[64];
+        static thread_local double2 kept[64];
+        if (memcmp(kept_f, rope->f, sizeof(kept_f)) != 0) {
+            for (int i = 0; i < 64; ++i) kept[i] = double2{cos(rope->f[i]), sin(rope->f[i])};
+            memcpy(kept_f, rope->f, sizeof(kept_f));
+        }
+        memcpy(a.step, kept, sizeof(kept));
+    }
     // all heads of a page in one workgroup, split where that leaves the chip's compute units without work
     const int hkv = c.n_kv_heads;
     const int64_t pages = int64_t(batch) * a.touched;
-    a.head_groups = int(std::min<int64_t>(hkv, std::max<int64_t>(1, 512 / std::max<int64_t>(pages, 1))));
+    a.head_groups = int(std::min<int64_t>(hkv, std::max<int64_t>(1, kAppendWorkgroups / pages)));
     const bool one_reader = a.touched == 1 && max_new == 1;
     if (one_reader) a.head_groups = 1;
     a.heads = (hkv + a.head_groups - 1) / a.head_groups;
@@ -320,7 +509,7 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     const int64_t blocks = pages * a.head_groups;
     if (blocks > 0x7fffffff) return fail(ST_ERR_SHAPE, "%s: grid too large", who);
     auto go = [&](auto kernel, int image) {
-        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * sizeof(double2) : 0) + size_t(2 * image);
+        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * (sizeof(double2) + (c.dtype == ST_BF16 ? 0 : sizeof(float2))) : 0) + size_t(2 * image);
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRowsThreads), smem, s, a);
     };
     // (LDS images: 16 tokens x D dims x HEADS heads, the same bytes for 64 dims and two heads as for 128 and one)
@@ -351,84 +540,113 @@ struct ReadArgs {
     int heads, head_groups;
 };
 
-// E8M0 as fp32 (255: NaN)
-__device__ __forceinline__ float e8m0(uint32_t b) { return __uint_as_float(b == 255u ? 0x7fc00000u : b << 23); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     bf16x2 r;
     r[0] = (__bf16)lo;
     r[1] = (__bf16)hi;
     return __builtin_bit_cast(uint32_t, r);
 }
-__device__ __forceinline__ float e2m1(uint32_t code) {
-    const uint32_t m = code & 7u;
-    const float v = m < 2 ? 0.5f * float(m) : ldexpf(float(2 + (m & 1u)), int(m >> 1) - 2);
-    return code & 8u ? -v : v;
+// the two codes of byte `byte` as bf16 times the power of two of an E8M0 byte (255: NaN), which the conversion reads in the exponent's place
+__device__ __forceinline__ uint32_t pair_of_codes(uint32_t w, uint32_t scale, int byte) {
+    const float s = __uint_as_float(scale << 23);
+    switch (byte) {
+        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    }
 }
 
-// A thread's share of a page of values of one head: eight values, at (slot, dim) of its own, as fp32 times the scale
-template <int FMT, int D, typename Each>
-__device__ __forceinline__ void read_values(const CacheView& cv, const uint8_t* page, int64_t page_head, int share, Each each) {
-    if constexpr (FMT == ST_MXFP4) {
-        // dword `share`: slots 4 q .. + 3 of dims 32 g + m and 32 g + 16 + m
-        constexpr int G = D / 32;
+// What a thread reads of a page of one head, ahead of its use: a share of the values (eight, at (slot, dim) of its own) and the eight dims 8 c .. of
+// the key of its slot, with their scales.
+template <int FMT, int D>
+struct Stored;
+
+template <int D>
+struct Stored<ST_MXFP4, D> {
+    static constexpr int G = D / 32;
+    uint32_t v, vs, k, ks;
+    __device__ __forceinline__ void load(const CacheView& cv, int64_t page_head, int share, int slot, int c) {
+        const uint8_t* kp = reinterpret_cast<const uint8_t*>(cv.k_pool) + page_head * (D * 8);
+        const uint8_t* vp = reinterpret_cast<const uint8_t*>(cv.v_pool) + page_head * (D * 8);
+        const uint8_t* sp = reinterpret_cast<const uint8_t*>(cv.k_scale) + page_head * D;
+        v = *reinterpret_cast<const uint32_t*>(vp + 4 * share);
+        vs = *reinterpret_cast<const uint32_t*>(sp + D / 2 + ((share / (16 * G)) * G + share % G) * 4);
+        k = *reinterpret_cast<const uint32_t*>(kp + ((c >> 2) * kPage + slot) * 16 + 4 * (c & 3));
+        ks = sp[(c >> 2) * kPage + slot];
+    }
+    // dword `share`: slots 4 q .. + 3 of dims 32 g + m and 32 g + 16 + m
+    template <typename Each>
+    __device__ __forceinline__ void values(int share, Each each) const {
         const int g = share % G, m = (share / G) % 16, q = share / (16 * G);
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(page + 4 * share);
-        const uint32_t sc = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(cv.k_scale) + page_head * D + D / 2 + (q * G + g) * 4);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const float scale = e8m0((sc >> (8 * t)) & 255u);
-            each(4 * q + t, 32 * g + m, e2m1((w >> (8 * t)) & 15u) * scale);
-            each(4 * q + t, 32 * g + 16 + m, e2m1((w >> (8 * t + 4)) & 15u) * scale);
-        }
-    } else {
-        // eight slots of dim share / 2
-        const int d = share / 2, s0 = 8 * (share & 1);
-        if constexpr (FMT == ST_FP8_E4M3) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(page + 8 * share);
-            const float* sc = cv.v_scale + page_head * kPage + s0;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                each(s0 + 4 * u, d, __builtin_amdgcn_cvt_f32_fp8(w[u], 0) * sc[4 * u]);
-                each(s0 + 4 * u + 1, d, __builtin_amdgcn_cvt_f32_fp8(w[u], 1) * sc[4 * u + 1]);
-                each(s0 + 4 * u + 2, d, __builtin_amdgcn_cvt_f32_fp8(w[u], 2) * sc[4 * u + 2]);
-                each(s0 + 4 * u + 3, d, __builtin_amdgcn_cvt_f32_fp8(w[u], 3) * sc[4 * u + 3]);
-            }
-        } else {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(page + 16 * share);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) each(s0 + e, d, bf16_bits_to_f32(uint16_t(w[e / 2] >> (16 * (e & 1)))));
+            const uint32_t w = pair_of_codes(v, (vs >> (8 * t)) & 255u, t);
+            each(4 * q + t, 32 * g + m, uint16_t(w));
+            each(4 * q + t, 32 * g + 16 + m, uint16_t(w >> 16));
         }
     }
-}
+    __device__ __forceinline__ u32x4 key() const { return u32x4{pair_of_codes(k, ks, 0), pair_of_codes(k, ks, 1), pair_of_codes(k, ks, 2), pair_of_codes(k, ks, 3)}; }
+};
 
-// eight dims (8 c ..) of a stored key
-template <int FMT, int D>
-__device__ __forceinline__ u32x4 read_key(const CacheView& cv, const uint8_t* page, int64_t page_head, int slot, int c) {
-    if constexpr (FMT == ST_MXFP4) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(page + ((c >> 2) * kPage + slot) * 16 + 4 * (c & 3));
-        const float scale = e8m0(reinterpret_cast<const uint8_t*>(cv.k_scale)[page_head * D + (c >> 2) * kPage + slot]);
-        u32x4 r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = pack_bf16(e2m1((w >> (8 * i)) & 15u) * scale, e2m1((w >> (8 * i + 4)) & 15u) * scale);
-        return r;
-    } else if constexpr (FMT == ST_FP8_E4M3) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(page + ((c >> 1) * kPage + slot) * 16 + 8 * (c & 1));
-        const float scale = cv.k_scale[page_head * kPage + slot];
-        u32x4 r;
+template <int D>
+struct Stored<ST_FP8_E4M3, D> {
+    u32x2 v, k;
+    f32x4 vs[2];
+    float ks;
+    __device__ __forceinline__ void load(const CacheView& cv, int64_t page_head, int share, int slot, int c) {
+        v = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(cv.v_pool) + page_head * (D * kPage) + 8 * share);
+        const f32x4* sc = reinterpret_cast<const f32x4*>(cv.v_scale + page_head * kPage + 8 * (share & 1));
+        vs[0] = sc[0];
+        vs[1] = sc[1];
+        k = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(cv.k_pool) + page_head * (D * kPage) + ((c >> 1) * kPage + slot) * 16 + 8 * (c & 1));
+        ks = cv.k_scale[page_head * kPage + slot];
+    }
+    static __device__ __forceinline__ void unpack(const u32x2& w, float (&f)[8]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            r[2 * u] = pack_bf16(__builtin_amdgcn_cvt_f32_fp8(w[u], 0) * scale, __builtin_amdgcn_cvt_f32_fp8(w[u], 1) * scale);
-            r[2 * u + 1] = pack_bf16(__builtin_amdgcn_cvt_f32_fp8(w[u], 2) * scale, __builtin_amdgcn_cvt_f32_fp8(w[u], 3) * scale);
+            f[4 * u] = __builtin_amdgcn_cvt_f32_fp8(w[u], 0);
+            f[4 * u + 1] = __builtin_amdgcn_cvt_f32_fp8(w[u], 1);
+            f[4 * u + 2] = __builtin_amdgcn_cvt_f32_fp8(w[u], 2);
+            f[4 * u + 3] = __builtin_amdgcn_cvt_f32_fp8(w[u], 3);
         }
-        return r;
-    } else {
-        return *reinterpret_cast<const u32x4*>(page + (c * kPage + slot) * 16);
     }
-}
+    // eight slots of dim share / 2
+    template <typename Each>
+    __device__ __forceinline__ void values(int share, Each each) const {
+        float f[8];
+        unpack(v, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) each(8 * (share & 1) + e, share / 2, f32_to_bf16_bits(f[e] * vs[e / 4][e & 3]));
+    }
+    __device__ __forceinline__ u32x4 key() const {
+        float f[8];
+        unpack(k, f);
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = pack_bf16(f[2 * i] * ks, f[2 * i + 1] * ks);
+        return r;
+    }
+};
+
+template <int D>
+struct Stored<ST_BF16, D> {
+    u32x4 v, k;
+    __device__ __forceinline__ void load(const CacheView& cv, int64_t page_head, int share, int slot, int c) {
+        v = *reinterpret_cast<const u32x4*>(cv.v_pool + page_head * (D * kPage) + 8 * share);
+        k = *reinterpret_cast<const u32x4*>(cv.k_pool + page_head * (D * kPage) + (c * kPage + slot) * 8);
+    }
+    template <typename Each>
+    __device__ __forceinline__ void values(int share, Each each) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) each(8 * (share & 1) + e, share / 2, uint16_t(v[e / 2] >> (16 * (e & 1))));
+    }
+    __device__ __forceinline__ u32x4 key() const { return k; }
+};
 
 template <int FMT, int D>
 __global__ __launch_bounds__(kRowsThreads) void read_rows_kernel(ReadArgs a) {
-    constexpr int L = D / 8, RP = kRowsThreads / L, HEADS = RP / kPage, IMAGE = D * kPage * Store<FMT, D>::PIECE / 8;
+    constexpr int L = D / 8, RP = kRowsThreads / L, HEADS = RP / kPage;
     constexpr int ROW = D + 8;                                   // (padded: slots start in different banks)
     __shared__ __align__(16) uint16_t s_v[2][HEADS][kPage][ROW];
     const int group = int(blockIdx.x) % a.head_groups, pi = (int(blockIdx.x) / a.head_groups) % a.touched, b = int(blockIdx.x) / (a.head_groups * a.touched);
@@ -445,21 +663,25 @@ __global__ __launch_bounds__(kRowsThreads) void read_rows_kernel(ReadArgs a) {
     const int share = int(threadIdx.x) % (L * kPage);            // of a head's page: D * 16 values / 8
     const int tok = page * kPage + slot;
     const bool wanted = tok >= lo && tok < hi;
+    // (the next heads' bytes are under way while these are sorted)
+    const int64_t first_head = int64_t(id) * a.cache.n_kv_heads + h0;
+    Stored<FMT, D> next;
+    if (sub < n_heads) next.load(a.cache, first_head + sub, share, slot, c);
     for (int h = 0, turn = 0; h < n_heads; h += HEADS, turn ^= 1) {
         const int mine = h + sub;
-        const int64_t page_head = int64_t(id) * a.cache.n_kv_heads + h0 + mine;
         const int64_t at = ((int64_t(b) * a.max_n + (tok - first)) * a.cache.n_kv_heads + h0 + mine) * D + 8 * c;
         if (mine < n_heads) {
-            read_values<FMT, D>(a.cache, reinterpret_cast<const uint8_t*>(a.cache.v_pool) + page_head * IMAGE, page_head, share,
-                                [&](int s, int d, float v) { s_v[turn][sub][s][d] = f32_to_bf16_bits(v); });
-            if (wanted)
-                *reinterpret_cast<u32x4*>(a.k_out + at) =
-                    read_key<FMT, D>(a.cache, reinterpret_cast<const uint8_t*>(a.cache.k_pool) + page_head * IMAGE, page_head, slot, c);
+            const Stored<FMT, D> now = next;
+            if (mine + HEADS < n_heads) next.load(a.cache, first_head + mine + HEADS, share, slot, c);
+            now.values(share, [&](int s, int d, uint16_t v) { s_v[turn][sub][s][d] = v; });
+            if (wanted) *reinterpret_cast<u32x4*>(a.k_out + at) = now.key();
         }
         __syncthreads();
         if (mine < n_heads && wanted) *reinterpret_cast<u32x4*>(a.v_out + at) = *reinterpret_cast<const u32x4*>(&s_v[turn][sub][slot][8 * c]);
     }
 }
+
+constexpr int kReadWorkgroups = 4096;
 
 // what both directions ask of a cache and of the rows beside it
 static st_status check_rows_call(const char* who, const st_dual_cache* caches, st_stream_kind which, const void* k, const void* v, int32_t max_rows,
@@ -522,7 +744,7 @@ extern "C" st_status st_kv_read(const st_dual_cache* caches, st_stream_kind whic
     a.touched = (max_n - 2 + kPage) / kPage + 1;
     const int64_t pages = int64_t(batch) * a.touched;
     const int hkv = c.n_kv_heads;
-    a.head_groups = int(std::min<int64_t>(hkv, std::max<int64_t>(1, 2048 / pages)));
+    a.head_groups = int(std::min<int64_t>(hkv, std::max<int64_t>(1, kReadWorkgroups / pages)));
     a.heads = (hkv + a.head_groups - 1) / a.head_groups;
     a.head_groups = (hkv + a.heads - 1) / a.heads;
     const int64_t blocks = pages * a.head_groups;
