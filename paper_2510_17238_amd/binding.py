@@ -106,7 +106,7 @@ def load_library():
     lib.st_rope_apply.argtypes = [vp, vp, vp, i64, i32, i32, f64, i32, vp]
     lib.st_rope_apply_qk.restype = i32
     lib.st_rope_apply_qk.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i32, f64, i32, vp]
-    spec = C.POINTER(RopeSpec)
+    spec = vp
     lib.st_norm_rope_apply_qk.restype = i32
     lib.st_norm_rope_apply_qk.argtypes = [vp, vp, i64, i32, vp, vp, vp, i64, i32, vp, vp, i64, i32, f64, spec, i32, vp]
     lib.st_norm_rope_bwd_workspace_bytes.restype = sz
@@ -322,43 +322,75 @@ def st_rope_apply_qk(q, k, positions, theta_base=1.0e6, q_out=None, k_out=None, 
 
 
 # ------------------------------------------------------- norm and rotation --
-def _token_rows(t, name, dtype=None):
-    """Token stride of t[n_tokens, heads, D], whose heads and dims are dense (a slice of a projection's output or a tensor of its own)."""
-    n, h, d = t.shape
-    if not t.is_cuda or (dtype is not None and t.dtype != dtype) or (h > 1 and t.stride(1) != d) or t.stride(2) != 1:
-        raise TypeError(f"{name} must be a device tensor [n_tokens, heads, head_dim] with dense heads, all tensors of one dtype")
-    return t.stride(0) if n > 1 else h * d
+def _launch_device(t, name):
+    """The device of t, which has to be the current one: the kernels run on the current device's stream."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise TypeError(f"{name} must be on the current GPU")
+    return dev
 
 
-def _norm_weight(w, x, name):
-    if w is not None and (not w.is_cuda or w.dtype != x.dtype or tuple(w.shape) != (x.shape[2],) or not w.is_contiguous()):
-        raise TypeError(f"{name} must be a contiguous device tensor [head_dim] of the rows' dtype")
-    return w
+def _launch_stream(stream, dev):
+    if stream is None:
+        return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+    return stream.cuda_stream
+
+
+def _rows_arg(t, name, dev, dtype, n, d):
+    """(heads, token stride) of t[n, heads, d], whose heads and dims are dense (a tensor of its own or a slice of a projection's output)."""
+    tokens, h, dim = t.shape
+    s0, s1, s2 = t.stride()
+    if t.dtype is not dtype or t.get_device() != dev or tokens != n or dim != d or (n > 0 and (s2 != 1 or (h > 1 and s1 != d))):
+        raise TypeError(f"{name} must be [n_tokens, heads, head_dim] with dense heads, of the dtype and on the device of the others")
+    return h, s0 if n > 1 else h * d
+
+
+def _weight_arg(w, name, dev, dtype, d):
+    if w is None:
+        return None
+    if w.dtype is not dtype or w.get_device() != dev or w.dim() != 1 or w.numel() != d or w.stride(0) != 1:
+        raise TypeError(f"{name} must be a contiguous tensor [head_dim] of the rows' dtype, on their device")
+    return w.data_ptr()
+
+
+def _positions_arg(t, dev, n):
+    if t.dtype is not torch.int32 or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise TypeError("positions must be a contiguous int32 tensor [n_tokens] on the rows' device")
+    return t.data_ptr()
+
+
+def _result(out, x, name, dev):
+    if out is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != dev or not out.is_contiguous():
+        raise TypeError(f"{name} must be dense, of the shape and dtype of its rows and on their device")
+    return out
 
 
 def st_norm_rope_apply_qk(q, k, q_weight, k_weight, positions, spec, eps=1.0e-6, q_out=None, k_out=None, stream=None):
     """q[n_tokens, Hq, D], k[n_tokens, Hkv, D] (or None) normalised per head (weights [D]; None: not normalised) and rotated by
     positions[n_tokens] as `spec` (RopeSpec) says -> (q_out, k_out).  q and k may be slices of one projection's output; outs default
     to new dense tensors."""
-    lib = load_library()
-    n, hq, d = q.shape
-    _dev_i32(positions, "positions")
-    assert positions.numel() == n
-    outs, args = [], []
-    for x, w, out, name in ((q, q_weight, q_out, "q"), (k, k_weight, k_out, "k")):
-        if x is None:
-            outs.append(None)
-            args += [None, None, 0, 0, None]
-            continue
-        assert x.shape[0] == n and x.shape[2] == d
-        stride = _token_rows(x, name, q.dtype)
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        assert out.is_cuda and out.shape == x.shape and out.dtype == x.dtype and out.is_contiguous()
-        outs.append(out)
-        args += [_ptr(out), _ptr(x), stride, x.shape[1], _ptr(_norm_weight(w, x, name + "_weight"))]
-    _check(lib.st_norm_rope_apply_qk(*args, _ptr(positions), n, d, float(eps), C.byref(spec), _dtype_code(q), _stream(stream)))
-    return tuple(outs)
+    lib = _lib or load_library()
+    n, _, d = q.shape
+    dtype, dev = q.dtype, _launch_device(q, "q")
+    hq, q_stride = _rows_arg(q, "q", dev, dtype, n, d)
+    qw = _weight_arg(q_weight, "q_weight", dev, dtype, d)
+    q_out = _result(q_out, q, "q_out", dev)
+    kp = ko = kw = None
+    hkv = k_stride = 0
+    if k is not None:
+        hkv, k_stride = _rows_arg(k, "k", dev, dtype, n, d)
+        kw = _weight_arg(k_weight, "k_weight", dev, dtype, d)
+        k_out = _result(k_out, k, "k_out", dev)
+        kp, ko = k.data_ptr(), k_out.data_ptr()
+    else:
+        k_out = None
+    status = lib.st_norm_rope_apply_qk(q_out.data_ptr(), q.data_ptr(), q_stride, hq, qw, ko, kp, k_stride, hkv, kw,
+                                       _positions_arg(positions, dev, n), n, d, eps, C.addressof(spec), _dtype_code(q), _launch_stream(stream, dev))
+    if status:
+        _check(status)
+    return q_out, k_out
 
 
 def st_norm_rope_bwd_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, head_dim):
@@ -370,10 +402,9 @@ def st_norm_rope_bwd_qk(d_q_out, d_k_out, q, k, q_weight, k_weight, positions, s
     """Gradients (dq, dk, dq_weight, dk_weight) of st_norm_rope_apply_qk; the weights' are fp32 [D], None without a weight or
     with weight_grads=False.  dq and dk may be slices of one gradient; a tensor without a weight may be None (as may k and d_k_out
     together: the queries alone)."""
-    lib = load_library()
+    lib = _lib or load_library()
     n, hq, d = d_q_out.shape
-    _dev_i32(positions, "positions")
-    assert positions.numel() == n
+    dtype, dev = d_q_out.dtype, _launch_device(d_q_out, "d_q_out")
     grads, sums, args = [], [], []
     for g, x, w, dx, name in ((d_q_out, q, q_weight, dq, "q"), (d_k_out, k, k_weight, dk, "k")):
         if g is None:
@@ -381,23 +412,31 @@ def st_norm_rope_bwd_qk(d_q_out, d_k_out, q, k, q_weight, k_weight, positions, s
             sums.append(None)
             args += [None, 0, None, None, None, 0, 0, None]
             continue
-        assert g.is_cuda and g.is_contiguous() and g.dtype == d_q_out.dtype and g.shape[0] == n and g.shape[2] == d
-        _norm_weight(w, g, name + "_weight")
-        stride = 0
+        h, _ = _rows_arg(g, "the gradient of " + name, dev, dtype, n, d)
+        if not g.is_contiguous():
+            raise TypeError(f"the gradient of {name}'s result must be dense")
+        stride, dx_stride = 0, h * d
         if x is not None:
-            assert x.shape == g.shape
-            stride = _token_rows(x, name, g.dtype)
+            hx, stride = _rows_arg(x, name, dev, dtype, n, d)
+            if hx != h:
+                raise TypeError(f"{name} and the gradient of its result differ in heads")
         if dx is None:
-            dx = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-        assert dx.shape == g.shape
+            dx = torch.empty(g.shape, dtype=dtype, device=g.device)
+        else:
+            hx, dx_stride = _rows_arg(dx, "d" + name, dev, dtype, n, d)
+            if hx != h:
+                raise TypeError(f"d{name} and the gradient of the result differ in heads")
+        wp = _weight_arg(w, name + "_weight", dev, dtype, d)
         dw = torch.empty(d, dtype=torch.float32, device=g.device) if w is not None and weight_grads else None
         grads.append(dx)
         sums.append(dw)
-        args += [_ptr(dx), _token_rows(dx, "d" + name, g.dtype), _ptr(dw), _ptr(g), _ptr(x), stride, g.shape[1], _ptr(w)]
-    if workspace is None and any(s is not None for s in sums):
+        args += [dx.data_ptr(), dx_stride, _ptr(dw), g.data_ptr(), _ptr(x), stride, h, wp]
+    if workspace is None and (sums[0] is not None or sums[1] is not None):
         workspace = _temp_workspace(st_norm_rope_bwd_workspace_bytes(n, hq, 0 if d_k_out is None else d_k_out.shape[1], d), d_q_out.device, stream)
-    _check(lib.st_norm_rope_bwd_qk(*args, _ptr(positions), n, d, float(eps), C.byref(spec), _dtype_code(d_q_out), _ptr(workspace),
-                                   0 if workspace is None else workspace.nbytes, _stream(stream)))
+    status = lib.st_norm_rope_bwd_qk(*args, _positions_arg(positions, dev, n), n, d, eps, C.addressof(spec), _dtype_code(d_q_out), _ptr(workspace),
+                                     0 if workspace is None else workspace.nbytes, _launch_stream(stream, dev))
+    if status:
+        _check(status)
     return (*grads, *sums)
 
 
@@ -675,15 +714,23 @@ def st_kv_append_rope(caches, which, k_new, v_new, theta_base, n_new=None, host_
     st_kv_append(caches, which, k_new, v_new, n_new, host_len_upper_bound, stream, rope_theta=theta_base)
 
 
-def _batch_rows(t, name, caches):
-    """Token stride of t[batch, tokens, Hkv, D], whose heads and dims are dense and whose sequences lie one behind the other."""
-    b, m, h, d = t.shape
-    if not t.is_cuda or t.dtype != torch.bfloat16 or h != caches.source.n_kv_heads or d != caches.source.head_dim or t.stride(3) != 1 or (h > 1 and t.stride(2) != d):
-        raise TypeError(f"{name} must be a bf16 device tensor [batch, tokens, n_kv_heads, head_dim] with dense heads")
-    stride = t.stride(1) if m > 1 else t.stride(0) if b > 1 and m == 1 else h * d
-    if b > 1 and m > 0 and t.stride(0) != m * stride:
-        raise TypeError(f"{name}: the sequences must lie one behind the other")
+def _batch_rows_arg(t, name, dev, batch, n, cache):
+    """Token stride of t[batch, n, Hkv, D], whose heads and dims are dense and whose sequences lie one behind the other."""
+    hkv, d = cache.n_kv_heads, cache.head_dim
+    s0, s1, s2, s3 = t.stride()
+    stride = s1 if n > 1 else s0 if batch > 1 and n == 1 else hkv * d
+    if t.dtype is not torch.bfloat16 or t.get_device() != dev or t.shape != (batch, n, hkv, d) or \
+            (n > 0 and (s3 != 1 or (hkv > 1 and s2 != d) or (batch > 1 and s0 != n * stride))):
+        raise TypeError(f"{name} must be bf16 [batch, tokens, n_kv_heads, head_dim] on the current GPU, heads dense, sequences one behind the other")
     return stride
+
+
+def _batch_i32_arg(t, name, dev, batch):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.get_device() != dev or t.numel() != batch or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous int32 tensor [batch] on the current GPU")
+    return t.data_ptr()
 
 
 def st_kv_append_norm_rope(caches, which, k_new, v_new, k_weight, spec, eps=1.0e-6, start_len=None, n_new=None, host_len_upper_bound=None,
@@ -691,38 +738,35 @@ def st_kv_append_norm_rope(caches, which, k_new, v_new, k_weight, spec, eps=1.0e
     """k_new, v_new: bf16 [batch, max_new, Hkv, D] (slices of a projection's output are fine) into a cache of any storage format; keys are
     normalised (k_weight [D] or None) and rotated by their index in the cache (spec: RopeSpec or None).  start_len: int32 [batch]
     device tensor, where the tokens go (None: behind what is there)."""
-    lib = load_library()
-    batch, max_new = k_new.shape[0], k_new.shape[1]
-    assert k_new.shape == v_new.shape
+    lib = _lib or load_library()
     cache = caches.source if which == ST_SOURCE else caches.reasoning
-    assert batch == cache.batch
-    if k_weight is not None and (not k_weight.is_cuda or k_weight.dtype != torch.bfloat16 or tuple(k_weight.shape) != (cache.head_dim,) or not k_weight.is_contiguous()):
-        raise TypeError("k_weight must be a contiguous bf16 device tensor [head_dim]")
-    for t, name in ((start_len, "start_len"), (n_new, "n_new")):
-        if t is not None:
-            assert _dev_i32(t, name).numel() == batch
+    batch, max_new = cache.batch, k_new.shape[1]
+    dev = _launch_device(k_new, "k_new")
     if host_len_upper_bound is None:
         host_len_upper_bound = cache.max_pages_per_seq * PAGE
-    st = caches.struct()
-    _check(lib.st_kv_append_norm_rope(C.byref(st), which, _ptr(k_new), _batch_rows(k_new, "k_new", caches), _ptr(v_new),
-                                      _batch_rows(v_new, "v_new", caches), _ptr(start_len), _ptr(n_new), max_new, batch,
-                                      int(host_len_upper_bound), _ptr(k_weight), float(eps), None if spec is None else C.byref(spec),
-                                      _stream(stream)))
+    status = lib.st_kv_append_norm_rope(C.byref(caches.struct()), which, k_new.data_ptr(), _batch_rows_arg(k_new, "k_new", dev, batch, max_new, cache),
+                                        v_new.data_ptr(), _batch_rows_arg(v_new, "v_new", dev, batch, max_new, cache),
+                                        _batch_i32_arg(start_len, "start_len", dev, batch), _batch_i32_arg(n_new, "n_new", dev, batch), max_new, batch,
+                                        int(host_len_upper_bound), _weight_arg(k_weight, "k_weight", dev, torch.bfloat16, cache.head_dim), eps,
+                                        None if spec is None else C.addressof(spec), _launch_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def st_kv_read(caches, which, k_out, v_out, first=None, n=None, stream=None):
     """Tokens first .. first + n - 1 (int32 [batch] device tensors; None: from 0, all that fit) of every sequence of a cache, as bf16 into
     k_out, v_out [batch, max_n, Hkv, D]; rows past n are left as they were.  Returns (k_out, v_out)."""
-    lib = load_library()
+    lib = _lib or load_library()
     cache = caches.source if which == ST_SOURCE else caches.reasoning
-    for t in (k_out, v_out):
-        assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 4
-        assert t.shape[0] == cache.batch and tuple(t.shape[2:]) == (cache.n_kv_heads, cache.head_dim) and t.shape[1] == k_out.shape[1]
-    for t, name in ((first, "first"), (n, "n")):
-        if t is not None:
-            assert _dev_i32(t, name).numel() == cache.batch
-    st = caches.struct()
-    _check(lib.st_kv_read(C.byref(st), which, _ptr(k_out), _ptr(v_out), _ptr(first), _ptr(n), k_out.shape[1], k_out.shape[0], _stream(stream)))
+    batch, max_n = cache.batch, k_out.shape[1]
+    dev = _launch_device(k_out, "k_out")
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t.dtype is not torch.bfloat16 or t.get_device() != dev or t.shape != (batch, max_n, cache.n_kv_heads, cache.head_dim) or not t.is_contiguous():
+            raise TypeError(f"{name} must be dense bf16 [batch, tokens, n_kv_heads, head_dim] on the current GPU")
+    status = lib.st_kv_read(C.byref(caches.struct()), which, k_out.data_ptr(), v_out.data_ptr(), _batch_i32_arg(first, "first", dev, batch),
+                            _batch_i32_arg(n, "n", dev, batch), max_n, batch, _launch_stream(stream, dev))
+    if status:
+        _check(status)
     return k_out, v_out
 
 

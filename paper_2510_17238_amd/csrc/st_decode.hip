@@ -1401,17 +1401,22 @@ static inline bool small_decode(int64_t batch, int hkv, int d, int max_src, int 
 // 455 with 4,096, 398 with 1,024; 8-bit, 32 / 8 heads 271 and 228; 20 of 3,000 + 900 tokens, 16 rows 78 with 4,096, 60 with 1,024;
 // but 64 of 700 + 700, 16 rows 85 with 512, 69 with a unit for each cache.  (Only the bounds are known here: a few long caches among
 // many short ones would take longer units, 128 of 300 tokens with one of 12,000 72 with 4,096 against 97.)
+// 4-bit caches: a quarter of the bytes per token, so the launch is over four times sooner and its end counts four times as much: 1,024 tokens
+// from 512 such units on, longer ones for 8,192 of them (2,048 with more than 8 rows) -- 16 sequences of up to 8K + 16K tokens, 32 / 8 heads of 128 dims
+// 56 with 1,024, 64 by the rule above; 64 of up to 8K + 24K 265 with 2,048, 268 with 1,024, 284 with 4,096; eight tokens of 64 of up to 8K + 16K 251 with 4,096, 290
+// with 1,024; 32 of 700 + 700 17.6 against 20.4 with 512; 4 of 4K + 8K 20.3 with 1,024, 19.4 with 512.
 // A few sequences are bound by the walk over a unit and not by bandwidth: 256 tokens up to 256 units of 512 (one sequence of 4K
 // tokens: 13.5 against 15.3), 128 up to 32 units (2K tokens: 11.7 against 15.3).
-static inline int decode_unit_tokens(int64_t batch, int hkv, int rows, int max_src, int max_rsn, int pinned, bool fp8 = false) {
+static inline int decode_unit_tokens(int64_t batch, int hkv, int rows, int max_src, int max_rsn, int pinned, bool fp8 = false, bool fp4 = false) {
     if (pinned) return pinned;               // the caller's choice (st_dual_lens::unit_tokens)
     auto per_head = [&](int unit) { return int64_t((max_src + unit - 1) / unit) + (max_rsn + unit - 1) / unit; };
     auto units = [&](int unit) { return batch * hkv * per_head(unit); };
     auto even = [&](int unit) { return 5 * per_head(unit) * std::min(unit, std::max(max_src, max_rsn)) <= 6 * (int64_t(max_src) + max_rsn); };
-    if (rows > 16 && units(kChunkLong) >= 192) return kChunkLong;
-    const int64_t enough = rows > 8 ? 384 : fp8 ? 768 : 2048;
+    if (!fp4 && rows > 16 && units(kChunkLong) >= 192) return kChunkLong;
+    const int64_t enough = fp4 ? (rows > 8 ? 2048 : 8192) : rows > 8 ? 384 : fp8 ? 768 : 2048;
     for (int unit = kChunkLong; unit > kChunk; unit /= 2)
         if (units(unit) >= enough && even(unit)) return unit;
+    if (fp4 && units(2 * kChunk) >= 512) return 2 * kChunk;
     return units(kChunk) > 256 ? kChunk : units(kChunk) > 32 ? kChunk / 2 : kChunkMin;
 }
 
@@ -1520,7 +1525,7 @@ static st_status decode_dual_impl(void* out, float* lse, const void* q, const st
     a.group = group;
     a.rows = lens->q_len * group;
     // Work unit: see decode_unit_tokens; a workspace sized for other length bounds may only hold longer units.
-    a.chunk = decode_unit_tokens(batch, hkv, a.rows, lens->max_src_len, lens->max_rsn_len, lens->unit_tokens, fp8 || fp4);
+    a.chunk = decode_unit_tokens(batch, hkv, a.rows, lens->max_src_len, lens->max_rsn_len, lens->unit_tokens, fp8, fp4);
     while (a.chunk < kChunk && decode_partial_bytes(a.chunk, batch, hkv, a.rows, d, lens->max_src_len, lens->max_rsn_len) > workspace_bytes)
         a.chunk *= 2;
     a.ncs = (lens->max_src_len + a.chunk - 1) / a.chunk;
