@@ -134,16 +134,20 @@ struct NormArgs {
 
 constexpr int kNormThreads = 256;
 
-// (cos, sin) times a of `count` tokens from tok0 on: s_cos[t * rot / 2 + i], s_sin likewise
+// (cos, sin) times a of `count` tokens from tok0 on: s_cos[t * rot / 2 + i], s_sin likewise.  The angle is reduced to an eighth of a turn in 64 bits:
+// rounded to 32 at up to half a turn it would be off by 1.2e-7 (fp32 rows 7.3e-8 of their norm away from 64 bits; so 6.2e-8).
 __device__ __forceinline__ void norm_table(const NormArgs& a, int64_t tok0, int count, float* s_cos, float* s_sin) {
     const int half = a.rope.rot / 2;
     for (int w = int(threadIdx.x); w < count * half; w += kNormThreads) {
         const int t = w / half, i = w - t * half;
-        const double rev = double(a.positions[tok0 + t]) * a.rope.f[i] * 0.15915494309189535;        // angle / 2 pi, reduced in 64 bits
+        const double rev = double(a.positions[tok0 + t]) * a.rope.f[i] * 0.15915494309189535;        // angle / 2 pi
+        const double turn = rev - rint(rev), quarter = rint(4.0 * turn);
+        const int n = int(quarter) & 3;
         float sn, cs;
-        sincosf(float((rev - rint(rev)) * 6.283185307179586), &sn, &cs);
-        s_cos[w] = cs * float(a.rope.a);
-        s_sin[w] = sn * float(a.rope.a);
+        sincosf(float((turn - 0.25 * quarter) * 6.283185307179586), &sn, &cs);
+        const float c = n & 1 ? sn : cs, s = n & 1 ? cs : sn, f = float(a.rope.a);
+        s_cos[w] = (n == 1 || n == 2 ? -c : c) * f;
+        s_sin[w] = (n >= 2 ? -s : s) * f;
     }
 }
 
@@ -353,14 +357,20 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_bwd_kernel(NormArgs a)
     }
 }
 
-// The workgroups' partial sums, 16 columns per workgroup: 64 groups of four lanes take every 64th row, in a fixed order.
+// The workgroups' partial sums, 16 columns per workgroup: 64 groups of four lanes take every 64th row, in a fixed order.  In 64 bits, which costs nothing
+// here: a thousand sums of either sign, added in 32, put as much error into the result as all the rows before.
 __global__ __launch_bounds__(256) void weight_sum_kernel(const float* __restrict__ part, int n_part, int dim, float* __restrict__ dqw,
                                                          float* __restrict__ dkw) {
-    __shared__ f32x4 s_sum[256];
+    typedef double f64x4 __attribute__((ext_vector_type(4)));
+    __shared__ f64x4 s_sum[256];
     const int col = int(blockIdx.x) * 16 + 4 * (int(threadIdx.x) & 3);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    f64x4 sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
-    for (int r = int(threadIdx.x) >> 2; r < n_part; r += 64) sum += *reinterpret_cast<const f32x4*>(part + int64_t(r) * 2 * dim + col);
+    for (int r = int(threadIdx.x) >> 2; r < n_part; r += 64) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(part + int64_t(r) * 2 * dim + col);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += double(x[e]);
+    }
     s_sum[threadIdx.x] = sum;
     __syncthreads();
     for (int n = 128; n >= 4; n >>= 1) {
@@ -371,7 +381,7 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(const float* __restrict
         float* dst = col < dim ? dqw : dkw;
         if (dst)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dst[col % dim + i] = s_sum[threadIdx.x][i];
+            for (int i = 0; i < 4; ++i) dst[col % dim + i] = float(s_sum[threadIdx.x][i]);
     }
 }
 
