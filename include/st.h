@@ -152,7 +152,7 @@ typedef struct st_rope_spec {
  *   q_weight, k_weight : [head_dim] of dtype dt, or NULL: that tensor is rotated without being normalised.
  *   n_kv_heads = 0 (k, k_out, k_weight ignored): the queries alone, as for a decoding step whose key goes through
  *              st_kv_append_norm_rope.
- *   positions : int32 [n_tokens], eps >= 0.
+ *   positions : int32 [n_tokens]; eps >= 0 and finite.  At most 65,536 heads of either kind.
  * fp32 arithmetic (the squares are summed in fp32: values up to 2^60), results rounded once.
  * ---------------------------------------------------------------------- */
 st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
@@ -165,7 +165,8 @@ st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, in
  *   q, k, q_stride, k_stride, weights, positions, eps, spec : the forward's (q or k may be NULL where its weight is NULL)
  *   dq, dk           : dL/dq, dL/dk with token strides dq_stride, dk_stride of their own (slices of the gradient of one
  *                      projection's output); may be d_q_out / d_k_out (dense) or q / k (same stride) themselves
- *   dq_weight, dk_weight : fp32 [head_dim] (written: the sum over all rows), or NULL where it is not wanted
+ *   dq_weight, dk_weight : fp32 [head_dim] (written: the sum over all rows), or NULL where it is not wanted; two arrays, also
+ *                      where one weight serves both tensors (its gradient is their sum)
  * workspace: at least st_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; not needed (may be NULL) without
  * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine.
  * With n_tokens = 0 the weight gradients are written as 0. */
@@ -466,14 +467,18 @@ st_status st_kv_append_rope(const st_dual_cache* caches, st_stream_kind which,
  *   k_new, v_new : bf16, token i of sequence b at element (b * max_new + i) * k_stride (v_stride), [n_kv_heads, head_dim]
  *                  dense there: slices of one projection's output are fine.  Strides are multiples of 8.
  *   start_len    : device int32 [batch], the index of each sequence's first new token; or NULL for the cache's
- *                  appended_len (then the call takes a second, tiny launch unless max_new is 1).  Given, it is authoritative: the tokens are stored at
- *                  start_len[b] .. and appended_len[b] becomes start_len[b] + n_new[b], so a caller can go back
- *                  to an earlier length (rejected drafts) and append there in one call; max_new = 0 sets the lengths alone.
+ *                  appended_len (then the call takes a second, tiny launch unless max_new is 1).  Given, it is authoritative:
+ *                  the tokens are stored at start_len[b] .. and appended_len[b] becomes start_len[b] + n_new[b], so a caller
+ *                  can go back to an earlier length (rejected drafts) and append there in one call; max_new = 0 sets the
+ *                  lengths alone.  n_new must not be appended_len then.
  *   n_new, max_new, batch, host_len_upper_bound, page tables, what is dropped: as for st_kv_append (the bound is on
  *                  start + n_new)
- *   k_weight     : bf16 [head_dim], or NULL: keys are not normalised.  eps >= 0.
+ *   k_weight     : bf16 [head_dim], or NULL: keys are not normalised.  eps >= 0 and finite.
  *   spec         : or NULL: keys are not rotated.
- * Keys are normalised and rotated in fp64 and rounded to bf16 once; codes are formed from those bf16 rows.
+ * Keys are normalised and rotated in fp64 and rounded to bf16 once; codes are formed from those bf16 rows (keys under
+ * 2^-100 in magnitude may be formed in fp32).  An undefined element of a row of an 8-bit cache is stored as such, beside the
+ * codes of the others.  As with st_kv_append, no byte of a token that is not new is written, and the call may run concurrently
+ * with a decode step that does not see the new ones.
  * ---------------------------------------------------------------------- */
 st_status st_kv_append_norm_rope(const st_dual_cache* caches, st_stream_kind which,
                                  const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,

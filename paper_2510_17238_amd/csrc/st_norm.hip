@@ -395,6 +395,13 @@ inline int bwd_workgroups(int64_t n_tokens) {
     return int(std::min<int64_t>(steps, kBwdWorkgroups));
 }
 
+// What both directions ask of the sizes.  (Rows of a workgroup are counted in 32 bits, rows of a call in 64.)
+static st_status check_sizes(const char* who, int64_t n_tokens, int n_q_heads, int n_kv_heads, double eps) {
+    if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
+    if (n_q_heads > (1 << 16) || n_kv_heads > (1 << 16) || n_tokens > (int64_t(1) << 40)) return fail(ST_ERR_SHAPE, "%s: more than 65,536 heads or 2^40 tokens", who);
+    if (!(eps >= 0.0 && eps < HUGE_VAL)) return fail(ST_ERR_INVALID_ARG, "%s: eps must be finite and not negative", who);
+    return ST_OK;
+}
 // what both directions ask of one tensor's arguments
 static st_status check_rows(const char* who, const char* name, const void* p, const void* w, int64_t stride, int heads, int head_dim, size_t size) {
     if (!p) return fail(ST_ERR_INVALID_ARG, "%s: %s is null", who, name);
@@ -418,8 +425,8 @@ extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q
     NormArgs a{};
     st_status r = make_rope_table(who, spec, head_dim, &a.rope);
     if (r != ST_OK) return r;
-    if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
-    if (!(eps >= 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    r = check_sizes(who, n_tokens, n_q_heads, n_kv_heads, eps);
+    if (r != ST_OK) return r;
     if (n_tokens == 0) return ST_OK;
     if (!positions) return fail(ST_ERR_INVALID_ARG, "%s: positions is null", who);
     const struct { void* out; const void* x; int64_t stride; int heads; const void* w; const char* name; } in[2] = {
@@ -472,8 +479,8 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     NormArgs a{};
     st_status r = make_rope_table(who, spec, head_dim, &a.rope);
     if (r != ST_OK) return r;
-    if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
-    if (!(eps >= 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    r = check_sizes(who, n_tokens, n_q_heads, n_kv_heads, eps);
+    if (r != ST_OK) return r;
     if (!positions && n_tokens > 0) return fail(ST_ERR_INVALID_ARG, "%s: positions is null", who);
     const struct { void* dx; int64_t dx_stride; float* dw; const void* g; const void* x; int64_t x_stride; int heads; const void* w; const char *name, *dname; } in[2] = {
         {dq, dq_stride, dq_weight, d_q_out, q, q_stride, n_q_heads, q_weight, "q", "dq"},
@@ -504,6 +511,7 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
         if (workspace_bytes < need) return fail(ST_ERR_CAPACITY, "%s: workspace has %zu bytes, needs %zu", who, workspace_bytes, need);
         a.part = static_cast<float*>(workspace);
     }
+    if (dq_weight && dq_weight == dk_weight) return fail(ST_ERR_INVALID_ARG, "%s: dq_weight and dk_weight are one array", who);
     a.positions = positions;
     a.n_tokens = n_tokens;
     a.eps = float(eps);

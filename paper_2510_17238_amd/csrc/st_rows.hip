@@ -81,12 +81,13 @@ __device__ __forceinline__ double inverse_root(double x) {
 
 constexpr int kScaleExpLeast = -100;             // of 8-bit rows and 4-bit blocks alike
 
-// Largest magnitude (as bf16 bits, non-finite above all) of a lane's eight values, over LANES neighbouring lanes
-template <int LANES>
+// Largest magnitude (as bf16 bits, non-finite above all, or left out) of a lane's eight values, over LANES neighbouring lanes
+template <int LANES, bool FINITE = false>
 __device__ __forceinline__ uint32_t row_top(const u32x4& x) {
     uint32_t top = 0;
+    auto magnitude = [](uint32_t m) { return FINITE && m >= 0x7f80u ? 0u : m; };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));
+    for (int i = 0; i < 4; ++i) top = max(top, max(magnitude(x[i] & 0x7fffu), magnitude((x[i] >> 16) & 0x7fffu)));
     auto fold = [&](auto ctrl) { top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), decltype(ctrl)::value, 0xf, 0xf, true))); };
     fold(std::integral_constant<int, 0xb1>{});
     fold(std::integral_constant<int, 0x4e>{});
@@ -127,10 +128,9 @@ struct Store<ST_FP8_E4M3, D> {
     };
     static __device__ __forceinline__ bool same(const Code& a, const Code& b) { return a.w[0] == b.w[0] && a.w[1] == b.w[1] && a.k == b.k; }
     static __device__ __forceinline__ Code encode(const u32x4& x) {
-        const uint32_t top = row_top<D / 8>(x);
+        // (448 = 1.75 * 2^8; an infinite or undefined element has a code of its own, the scale is the others')
         Code r;
-        // (448 = 1.75 * 2^8.  A row with an infinite or undefined element: that element's code is NaN, the scale the largest there is)
-        r.k = scale_exponent(min(top, 0x7f7fu), 96, 8);
+        r.k = scale_exponent(row_top<D / 8, true>(x), 96, 8);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float f[4];
@@ -394,6 +394,10 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
         }
         __syncthreads();
     }
+    // (32 bits hold a key's interval if no product of its weight with something lost below 2^-126 counts: weights to 2^20, and what is lost is under 2^-105)
+    bool usual = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) usual = usual && (w_raw[i] & 0x7fffu) <= 0x4980u && ((w_raw[i] >> 16) & 0x7fffu) <= 0x4980u;
     auto load = [&](const uint16_t* src, int64_t stride, int t, int h) { return *reinterpret_cast<const u32x4*>(src + (tok0 + t) * stride + (h0 + h) * D + 8 * c); };
     auto page_of = [&](uint16_t* pool, int h) { return reinterpret_cast<uint8_t*>(pool) + (int64_t(id) * a.cache.n_kv_heads + h0 + h) * IMAGE; };
     auto key = [&](const u32x4& raw, int t) -> typename S::Code {
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
             u32x4 x_lo, x_hi;
             const bool sure = quick_key<D>(raw, a, w_raw, s_cos + t * half, s_sin + t * half, x_lo, x_hi);
             const typename S::Code c_lo = S::encode(x_lo), c_hi = S::encode(x_hi);
-            if (!__any(!sure || !S::same(c_lo, c_hi))) return c_lo;          // (else one wave in some tens)
+            if (!__any(!usual || !sure || !S::same(c_lo, c_hi))) return c_lo;          // (else one wave in some tens)
         }
         return S::encode(exact_key<D>(raw, a, w_raw, table + t * half));
     };
@@ -467,6 +471,11 @@ __global__ void append_rows_len_kernel(int32_t* __restrict__ appended_len, const
     appended_len[b] = start + min(n, capacity - start);
 }
 
+// pages of a sequence that n consecutive tokens may touch: the first of them in a page's last slot at worst, and no more than there are
+inline int pages_touched(int n, const st_kv_cache& c) {
+    return int(std::min<int64_t>((int64_t(n) - 2 + kPage) / kPage + 1, c.max_pages_per_seq));
+}
+
 constexpr int kAppendWorkgroups = 2048;
 
 st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
@@ -481,7 +490,7 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     a.start_len = start_len;
     a.n_new = n_new;
     a.max_new = max_new;
-    a.touched = (max_new - 2 + kPage) / kPage + 1;               // (the first token in a page's last slot at worst)
+    a.touched = pages_touched(max_new, c);
     a.k_weight = static_cast<const uint16_t*>(k_weight);
     a.eps = eps;
     a.rotate = rope != nullptr;
@@ -523,7 +532,7 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     }
     ST_LAUNCH_CHECK("append_rows_kernel");
     if (!a.write_len) {
-        hipLaunchKernelGGL(append_rows_len_kernel, dim3((batch + 255) / 256), dim3(256), 0, s, c.appended_len, n_new, max_new, batch, c.max_pages_per_seq * kPage);
+        hipLaunchKernelGGL(append_rows_len_kernel, dim3((unsigned(batch) + 255u) / 256u), dim3(256), 0, s, c.appended_len, n_new, max_new, batch, c.max_pages_per_seq * kPage);
         ST_LAUNCH_CHECK("append_rows_len_kernel");
     }
     return ST_OK;
@@ -709,6 +718,7 @@ extern "C" st_status st_kv_append_norm_rope(const st_dual_cache* caches, st_stre
     const st_kv_cache& c = which == ST_SOURCE ? caches->source : caches->reasoning;
     if (!c.appended_len) return fail(ST_ERR_INVALID_ARG, "%s: appended_len is null", who);
     if (start_len == c.appended_len) start_len = nullptr;       // (the same lengths, which the call is about to change)
+    if (start_len && n_new == c.appended_len) return fail(ST_ERR_INVALID_ARG, "%s: n_new is the cache's appended_len, which the call writes", who);
     const int64_t dense = int64_t(c.n_kv_heads) * c.head_dim;
     if (k_stride < dense || v_stride < dense) return fail(ST_ERR_SHAPE, "%s: a token stride of %lld elements for %d heads of %d", who, (long long)std::min(k_stride, v_stride), c.n_kv_heads, c.head_dim);
     if (k_stride % 8 != 0 || v_stride % 8 != 0) return fail(ST_ERR_INVALID_ARG, "%s: token strides must be multiples of 16 bytes", who);
@@ -716,7 +726,7 @@ extern "C" st_status st_kv_append_norm_rope(const st_dual_cache* caches, st_stre
     if (host_len_upper_bound < 0 || host_len_upper_bound > capacity)
         return fail(ST_ERR_CAPACITY, "%s: length bound %d exceeds the page table (%lld tokens per sequence)", who, host_len_upper_bound, (long long)capacity);
     if (!aligned16(k_weight)) return fail(ST_ERR_INVALID_ARG, "%s: k_weight must be 16-byte aligned", who);
-    if (!(eps >= 0.0)) return fail(ST_ERR_INVALID_ARG, "%s: eps must not be negative", who);
+    if (!(eps >= 0.0 && eps < HUGE_VAL)) return fail(ST_ERR_INVALID_ARG, "%s: eps must be finite and not negative", who);
     RopeTable rope;
     if (spec) {
         r = make_rope_table(who, spec, c.head_dim, &rope);
@@ -741,7 +751,7 @@ extern "C" st_status st_kv_read(const st_dual_cache* caches, st_stream_kind whic
     a.first = first;
     a.n = n;
     a.max_n = max_n;
-    a.touched = (max_n - 2 + kPage) / kPage + 1;
+    a.touched = pages_touched(max_n, c);
     const int64_t pages = int64_t(batch) * a.touched;
     const int hkv = c.n_kv_heads;
     a.head_groups = int(std::min<int64_t>(hkv, std::max<int64_t>(1, kReadWorkgroups / pages)));

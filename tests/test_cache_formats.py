@@ -51,6 +51,16 @@ def test_append_refusals(lib):
     assert lib.st_kv_append_norm_rope(None, 0, FAKE, 256, FAKE, 256, None, None, 8, 1, 64, None, 0.0, None, None) == 1
 
 
+def test_append_refuses_lengths_that_it_writes(lib):
+    import paper_2510_17238_amd.binding as B
+    c = dual(B)
+    own = c.source.appended_len
+    call = lambda start, n: lib.st_kv_append_norm_rope(C.byref(c), B.ST_SOURCE, FAKE, 256, FAKE, 256, start, n, 8, 1, 65, None, 0.0, None, None)
+    assert call(0x7000, own) == 1 and b"appended_len" in lib.st_last_error()
+    assert call(None, own) == 4 and call(own, own) == 4                     # read before they are written: on to the next check
+    assert append(lib, B, eps=float("inf")) == 1
+
+
 def test_read_refusals(lib):
     import paper_2510_17238_amd.binding as B
 

@@ -1,4 +1,6 @@
 """New tokens' rows into paged caches of every storage format -- normalised, rotated, coded -- and rows read back."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -132,6 +134,85 @@ def test_plain_rows_as_by_the_plain_append(st, store, hkv, d, batch, chunks):
             want = stored(store, x)
             assert np.array_equal(f64(got[i, :lens[i]]), want), (i, which)
         assert bool((k_all[i, lens[i]:] == 9.0).all()) and bool((v_all[i, lens[i]:] == -9.0).all())
+
+
+@pytest.mark.gpu
+def test_undefined_elements_of_8_bit_rows(st):
+    """An undefined element of an 8-bit row leaves the others as they are: what st_kv_append stores."""
+    rng, g = np.random.default_rng(6), gen(6)
+    a, _ = cache_of(st, rng, "fp8", 2, 2, 3, 128)
+    b = st.KVCache(a.n_pages, 2, 2, 3, 128, a.page_table, fill=0xab, fp8=True)
+    k, v = rand_rows(g, 2, 21, 3, 128), rand_rows(g, 2, 21, 3, 128)
+    k[0, 2, 1, 77], k[1, 20, 0, 0], v[1, 3, 2, 127] = float("nan"), float("nan"), float("nan")
+    st.st_kv_append(pair(st, a), st.ST_SOURCE, k, v)
+    st.st_kv_append_norm_rope(pair(st, b), st.ST_SOURCE, k, v, None, None)
+    for x, y in ((a.k_pool, b.k_pool), (a.v_pool, b.v_pool), (a.k_scale.view(torch.int32), b.k_scale.view(torch.int32)), (a.v_scale.view(torch.int32), b.v_scale.view(torch.int32))):
+        assert torch.equal(x, y)
+    got, _ = read(st, pair(st, b), st.ST_SOURCE, 2, 21)
+    assert int(torch.isnan(got).sum()) == 2
+    # rotated as well: the element's pair
+    spec, _ = spec_of(st)
+    st.st_kv_append_norm_rope(pair(st, b), st.ST_SOURCE, k, v, None, spec, start_len=torch.zeros(2, dtype=torch.int32, device=DEV))
+    got, _ = read(st, pair(st, b), st.ST_SOURCE, 2, 21)
+    assert int(torch.isnan(got).sum()) == 4 and bool(torch.isnan(got[0, 2, 1, 13])) and bool(torch.isnan(got[0, 2, 1, 77]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("store", FORMATS)
+def test_undefined_and_huge_keys_through_the_norm(st, store):
+    """Rows that 32 bits do not hold are formed in 64: elements of 2^70, of 2^-70 without eps, an undefined element (its whole row)."""
+    d, n = 128, 24
+    g = gen(7)
+    c, _ = cache_of(st, np.random.default_rng(7), store, 1, 2, 1, d)
+    x = torch.randn((1, n, 1, d), generator=g, device=DEV)
+    x[0, 1::3] *= 2.0 ** 70
+    x[0, 2::3] *= 2.0 ** -70
+    x = x.to(torch.bfloat16)
+    x[0, 5, 0, 9] = float("nan")
+    w = (1.0 + 0.3 * torch.randn(d, generator=g, device=DEV)).to(torch.bfloat16)
+    spec, rope = spec_of(st)
+    st.st_kv_append_norm_rope(pair(st, c), st.ST_SOURCE, x, x, w, spec, eps=0.0)
+    k, _ = read(st, pair(st, c), st.ST_SOURCE, 1, n)
+    rows = [i for i in range(n) if i != 5]
+    want = stored(store, L.bf16(L.norm_rope(f64(x)[0][rows], f64(w), np.array(rows), 0.0, *rope)))
+    assert np.array_equal(f64(k)[0][rows], want) and bool(torch.isnan(k[0, 5]).all())
+
+
+@pytest.mark.gpu
+def test_unusual_weights(st):
+    """Weights up to 2^100 on elements that the row's norm has made as small: products that 32 bits lose on the way."""
+    d, n = 128, 16
+    g = gen(8)
+    x = torch.randn((1, n, 1, d), generator=g, device=DEV)
+    x[..., 1::2] *= 2.0 ** -128                                  # bf16 values of few bits, below the smallest normal number
+    w = 1.0 + 0.3 * torch.randn(d, generator=g, device=DEV)
+    w[1::2] *= 2.0 ** 125
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    spec, rope = spec_of(st)
+    for store in FORMATS:
+        c, _ = cache_of(st, np.random.default_rng(8), store, 1, 2, 1, d)
+        st.st_kv_append_norm_rope(pair(st, c), st.ST_SOURCE, x, x, w, spec, eps=1e-6)
+        k, _ = read(st, pair(st, c), st.ST_SOURCE, 1, n)
+        assert np.array_equal(f64(k)[0], stored(store, L.bf16(L.norm_rope(f64(x)[0], f64(w), np.arange(n), 1e-6, *rope))))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("store", FORMATS)
+def test_rows_for_more_tokens_than_there_are_pages(st, store):
+    """max_new and max_n are strides and bounds: up to the largest number, whatever the page table holds."""
+    B = st.binding
+    d, most = 64, 2 ** 31 - 1
+    c, _ = cache_of(st, np.random.default_rng(9), store, 1, 2, 2, d)
+    dual, lib, p = pair(st, c), B.load_library(), lambda t: t.data_ptr()
+    k, v = rand_rows(gen(9), 1, 21, 2, d), rand_rows(gen(10), 1, 21, 2, d)
+    n = torch.tensor([21], dtype=torch.int32, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.st_kv_append_norm_rope(C.byref(dual.struct()), st.ST_SOURCE, p(k), 2 * d, p(v), 2 * d, None, p(n), most, 1, 32, None, 0.0, None, stream) == 0
+    assert int(c.appended_len[0]) == 21
+    out = [torch.full((1, 22, 2, d), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    assert lib.st_kv_read(C.byref(dual.struct()), st.ST_SOURCE, p(out[0]), p(out[1]), None, p(n), most, 1, stream) == 0
+    for got, want in zip(out, (k, v)):
+        assert np.array_equal(f64(got)[0, :21], stored(store, f64(want)[0])) and bool((got[0, 21] == 7.0).all())
 
 
 SPECS = [dict(), dict(layout="interleaved"), dict(rotary=32, scaling="linear", factor=3.0), dict(rotary=48, scaling="ntk", factor=2.0),

@@ -118,6 +118,19 @@ def test_gradient_refusals(lib):
         assert b"st_norm_rope_bwd_qk" in lib.st_last_error()
 
 
+def test_refusals_of_sizes_and_shared_results(lib):
+    import paper_2510_17238_amd.binding as B
+    for code, kw in [(2, dict(hq=65537, qs=65537 * 128)), (2, dict(hkv=65537, ks=65537 * 128)), (2, dict(n=2 ** 40 + 1)), (1, dict(eps=float("inf")))]:
+        assert _fwd(lib, B, **kw) == code, (kw, lib.st_last_error())
+    spec = B.RopeSpec()
+
+    def bwd(dwq, dwk, hkv=2, eps=1e-6):
+        return lib.st_norm_rope_bwd_qk(0x2000, 512, dwq, FAKE, FAKE, 512, 4, FAKE, 0x4000, 256, dwk, FAKE, FAKE, 256, hkv, FAKE, FAKE, 5, 128, eps, C.byref(spec),
+                                       B.ST_BF16, FAKE, 1 << 20, None)
+    assert bwd(0x8000, 0x8000) == 1 and b"one array" in lib.st_last_error()
+    assert bwd(0x8000, 0x9000, hkv=65537) == 2 and bwd(0x8000, 0x9000, eps=float("inf")) == 1
+
+
 def test_binding_refusals():
     import torch
     import paper_2510_17238_amd as st
