@@ -198,6 +198,7 @@ def _ptr(t):
 # the handle of torch's current stream without building a Stream object around it, which takes longer than the rest of a
 # short call's arguments together (2.5 of 11 us for a decoding step)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)     # (with a GPU tensor in hand the runtime is up)
 
 
 def _stream(stream):
@@ -325,7 +326,7 @@ def st_rope_apply_qk(q, k, positions, theta_base=1.0e6, q_out=None, k_out=None, 
 def _launch_device(t, name):
     """The device of t, which has to be the current one: the kernels run on the current device's stream."""
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current_device():
         raise TypeError(f"{name} must be on the current GPU")
     return dev
 
@@ -359,9 +360,17 @@ def _positions_arg(t, dev, n):
     return t.data_ptr()
 
 
-def _result(out, x, name, dev):
+def _new(shape, dtype, device, stream):
+    """A result nobody gave: of the stream that the kernels are launched on, as if the call stood under torch.cuda.stream(stream)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _result(out, x, name, dev, stream):
     if out is None:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return _new(x.shape, x.dtype, x.device, stream)
     if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != dev or not out.is_contiguous():
         raise TypeError(f"{name} must be dense, of the shape and dtype of its rows and on their device")
     return out
@@ -376,13 +385,13 @@ def st_norm_rope_apply_qk(q, k, q_weight, k_weight, positions, spec, eps=1.0e-6,
     dtype, dev = q.dtype, _launch_device(q, "q")
     hq, q_stride = _rows_arg(q, "q", dev, dtype, n, d)
     qw = _weight_arg(q_weight, "q_weight", dev, dtype, d)
-    q_out = _result(q_out, q, "q_out", dev)
+    q_out = _result(q_out, q, "q_out", dev, stream)
     kp = ko = kw = None
     hkv = k_stride = 0
     if k is not None:
         hkv, k_stride = _rows_arg(k, "k", dev, dtype, n, d)
         kw = _weight_arg(k_weight, "k_weight", dev, dtype, d)
-        k_out = _result(k_out, k, "k_out", dev)
+        k_out = _result(k_out, k, "k_out", dev, stream)
         kp, ko = k.data_ptr(), k_out.data_ptr()
     else:
         k_out = None
@@ -421,13 +430,13 @@ def st_norm_rope_bwd_qk(d_q_out, d_k_out, q, k, q_weight, k_weight, positions, s
             if hx != h:
                 raise TypeError(f"{name} and the gradient of its result differ in heads")
         if dx is None:
-            dx = torch.empty(g.shape, dtype=dtype, device=g.device)
+            dx = _new(g.shape, dtype, g.device, stream)
         else:
             hx, dx_stride = _rows_arg(dx, "d" + name, dev, dtype, n, d)
             if hx != h:
                 raise TypeError(f"d{name} and the gradient of the result differ in heads")
         wp = _weight_arg(w, name + "_weight", dev, dtype, d)
-        dw = torch.empty(d, dtype=torch.float32, device=g.device) if w is not None and weight_grads else None
+        dw = _new(d, torch.float32, g.device, stream) if w is not None and weight_grads else None
         grads.append(dx)
         sums.append(dw)
         args += [dx.data_ptr(), dx_stride, _ptr(dw), g.data_ptr(), _ptr(x), stride, h, wp]

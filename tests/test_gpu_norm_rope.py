@@ -241,6 +241,29 @@ def test_other_stream_and_graph_replays(st):
 
 
 @pytest.mark.gpu
+def test_results_are_of_the_stream_of_the_call(st):
+    """stream=: memory that the current stream has just let go, with work on it still under way, is not where the results go."""
+    n, hq, hkv, d = 4096, 16, 8, 128
+    q, k, wq, wk, pos = inputs("bf16", n, hq, hkv, d, True, 14)
+    sp, _ = spec_of(st)
+    gq, gk = torch.randn((n, hq, d), device=DEV).bfloat16(), torch.randn((n, hkv, d), device=DEV).bfloat16()
+    both = lambda **kw: [*st.st_norm_rope_apply_qk(q, k, wq, wk, pos, sp, **kw), *st.st_norm_rope_bwd_qk(gq, gk, q, k, wq, wk, pos, sp, **kw)]
+    ref = both()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    slow = torch.randn((4096, 4096), device=DEV)
+    for shape, dtype in [(x.shape, x.dtype) for x in ref]:
+        y = torch.empty(shape, dtype=dtype, device=DEV)
+        for _ in range(4):
+            slow @ slow
+        y.fill_(7.0)
+        del y
+    got = both(stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+@pytest.mark.gpu
 def test_rotation_alone_is_the_plain_rotation(st):
     """Without weights and with the plain spec: st_rope_apply_qk within a step of the result's type."""
     q, k, _, _, pos = inputs("bf16", 200, 8, 4, 128, False, 2)
