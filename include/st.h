@@ -391,7 +391,8 @@ st_status st_attn_prefill_bwd(void* dq, void* dk, void* dv, const void* d_out, c
  * -100) for which the block's largest magnitude is at most 6 * 2^k, with the byte k + 127 beside it (k = 0 for an all-zero
  * block).  The division is exact, the rounding is to nearest, ties to the even code.  A block with an infinite or undefined
  * element has scale byte 255 and reads as NaN as a whole; values of 2^127 and above may read as infinite.
- * 4.25 bits per element.  Layouts, in bytes, chosen so that one 16-byte load per lane is a matrix-core operand:
+ * 4.25 bits per element.  Every byte belongs to one token: tokens may be stored beside a decode step that does not see them, as in the
+ * other formats.  Layouts, in bytes, chosen so that one 16-byte load per lane is a matrix-core operand:
  *   k_pool : [n_pages][n_kv_heads][head_dim / 32][16 slots][16]    element (page,h,slot,d) is nibble d % 2 of byte (d % 32) / 2
  *   v_pool : [n_pages][n_kv_heads][4][16][head_dim / 32][4]        element (page,h,slot,d) is nibble (d / 16) % 2 of byte
  *            [slot / 4][d % 16][d / 32][slot % 4]

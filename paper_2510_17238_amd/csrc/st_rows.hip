@@ -10,6 +10,11 @@
 // as wide as a sixth of its block's largest value: 32 bits would put a few keys of every million on the other side of the line between two codes,
 // and the same row would not always be stored alike.  Nearly every row's codes are the same at both ends of the interval that 32-bit arithmetic
 // leaves, though, and those rows are done with it (quick_key).
+//
+// Measured, 4 bits, 8 heads of 128 dims.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 74 us, the rows of a cache
+// without norm and rotation in 56, read back in 59, one after the other in 120; nothing between the loads and the stores but the codes, loads
+// two to eight passes ahead, rows in the order in which they lie, 40 vector instructions less of 379 per pass: each within 3 % of that, so it is
+// memory (at the rate of a large copy 45).  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 5.4 and 3.0.
 #include <math.h>
 #include <string.h>
 
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
             u32x4 x_lo, x_hi;
             const bool sure = quick_key<D>(raw, a, w_raw, s_cos + t * half, s_sin + t * half, x_lo, x_hi);
             const typename S::Code c_lo = S::encode(x_lo), c_hi = S::encode(x_hi);
-            if (!__any(!usual || !sure || !S::same(c_lo, c_hi))) return c_lo;          // (else one wave in some tens)
+            if (!__any(!usual || !sure || !S::same(c_lo, c_hi))) return c_lo;          // (seldom otherwise)
         }
         return S::encode(exact_key<D>(raw, a, w_raw, table + t * half));
     };
@@ -476,6 +481,8 @@ inline int pages_touched(int n, const st_kv_cache& c) {
     return int(std::min<int64_t>((int64_t(n) - 2 + kPage) / kPage + 1, c.max_pages_per_seq));
 }
 
+// Workgroups to aim at by splitting the heads of a page: 64 sentences of up to 190 tokens (900 pages) 17 us, with 512 24, with 4,096 19 (the page's
+// angles are evaluated by each).
 constexpr int kAppendWorkgroups = 2048;
 
 st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
@@ -690,6 +697,7 @@ __global__ __launch_bounds__(kRowsThreads) void read_rows_kernel(ReadArgs a) {
     }
 }
 
+// (There are no angles to share: the same sentences are read in 9.9 us, with 8,192 in 11.5.)
 constexpr int kReadWorkgroups = 4096;
 
 // what both directions ask of a cache and of the rows beside it
