@@ -734,6 +734,11 @@ def _batch_rows_arg(t, name, dev, batch, n, cache):
     return stride
 
 
+def _cache_device(cache, dev):
+    if cache.k_pool.get_device() != dev or cache.page_table.get_device() != dev:
+        raise TypeError("the cache must be on the current GPU")
+
+
 def _batch_i32_arg(t, name, dev, batch):
     if t is None:
         return None
@@ -751,6 +756,7 @@ def st_kv_append_norm_rope(caches, which, k_new, v_new, k_weight, spec, eps=1.0e
     cache = caches.source if which == ST_SOURCE else caches.reasoning
     batch, max_new = cache.batch, k_new.shape[1]
     dev = _launch_device(k_new, "k_new")
+    _cache_device(cache, dev)
     if host_len_upper_bound is None:
         host_len_upper_bound = cache.max_pages_per_seq * PAGE
     status = lib.st_kv_append_norm_rope(C.byref(caches.struct()), which, k_new.data_ptr(), _batch_rows_arg(k_new, "k_new", dev, batch, max_new, cache),
@@ -769,6 +775,7 @@ def st_kv_read(caches, which, k_out, v_out, first=None, n=None, stream=None):
     cache = caches.source if which == ST_SOURCE else caches.reasoning
     batch, max_n = cache.batch, k_out.shape[1]
     dev = _launch_device(k_out, "k_out")
+    _cache_device(cache, dev)
     for t, name in ((k_out, "k_out"), (v_out, "v_out")):
         if t.dtype is not torch.bfloat16 or t.get_device() != dev or t.shape != (batch, max_n, cache.n_kv_heads, cache.head_dim) or not t.is_contiguous():
             raise TypeError(f"{name} must be dense bf16 [batch, tokens, n_kv_heads, head_dim] on the current GPU")

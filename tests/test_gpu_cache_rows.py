@@ -215,6 +215,28 @@ def test_rows_for_more_tokens_than_there_are_pages(st, store):
         assert np.array_equal(f64(got)[0, :21], stored(store, f64(want)[0])) and bool((got[0, 21] == 7.0).all())
 
 
+@pytest.mark.gpu
+def test_binding_refuses_what_the_kernels_cannot_take(st):
+    c, table = cache_of(st, np.random.default_rng(3), "mxfp4", 2, 2, 2, 64)
+    k = torch.zeros((2, 5, 2, 64), dtype=torch.bfloat16, device=DEV)
+    i = torch.zeros(2, dtype=torch.int32, device=DEV)
+    away = st.KVCache(c.n_pages, 2, 2, 2, 64, c.page_table, device="cpu", mxfp4=True)          # pools in host memory
+    append = lambda cache=c, k=k, v=k, w=None, **kw: st.st_kv_append_norm_rope(pair(st, cache), st.ST_SOURCE, k, v, w, None, **kw)
+    read = lambda cache=c, k=k, v=k.clone(), **kw: st.st_kv_read(pair(st, cache), st.ST_SOURCE, k, v, **kw)
+    for call in (append, read):
+        for bad in (dict(cache=away), dict(k=k.cpu()), dict(v=k.float()), dict(v=k[:, :4]), dict(k=k[:1])):
+            with pytest.raises(TypeError):
+                call(**bad)
+    for bad in (dict(w=torch.ones(64, device=DEV)), dict(w=torch.ones(32, dtype=torch.bfloat16, device=DEV)), dict(start_len=i.long()), dict(n_new=i[:1]),
+                dict(start_len=i.cpu()), dict(k=k.transpose(2, 3).contiguous().transpose(2, 3))):
+        with pytest.raises(TypeError):
+            append(**bad)
+    for bad in (dict(first=i.long()), dict(n=i[:1]), dict(k=k.repeat(1, 2, 1, 1)[:, ::2])):
+        with pytest.raises(TypeError):
+            read(**bad)
+    assert int(c.appended_len.abs().sum()) == 0
+
+
 SPECS = [dict(), dict(layout="interleaved"), dict(rotary=32, scaling="linear", factor=3.0), dict(rotary=48, scaling="ntk", factor=2.0),
          dict(scaling="yarn", factor=4.0, original=4096), dict(layout="interleaved", rotary=16, scaling="yarn", factor=8.0, original=4096, attention=0.9)]
 
