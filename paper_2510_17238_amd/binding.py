@@ -338,12 +338,13 @@ def _launch_stream(stream, dev):
 
 
 def _rows_arg(t, name, dev, dtype, n, d):
-    """(heads, token stride) of t[n, heads, d], whose heads and dims are dense (a tensor of its own or a slice of a projection's output)."""
-    tokens, h, dim = t.shape
+    """(shape, token stride) of t[n, heads, d], whose heads and dims are dense (a tensor of its own or a slice of a projection's output)."""
+    shape = t.shape
+    tokens, h, dim = shape
     s0, s1, s2 = t.stride()
     if t.dtype is not dtype or t.get_device() != dev or tokens != n or dim != d or (n > 0 and (s2 != 1 or (h > 1 and s1 != d))):
         raise TypeError(f"{name} must be [n_tokens, heads, head_dim] with dense heads, of the dtype and on the device of the others")
-    return h, s0 if n > 1 else h * d
+    return shape, s0 if n > 1 else h * d
 
 
 def _weight_arg(w, name, dev, dtype, d):
@@ -368,10 +369,10 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _result(out, x, name, dev, stream):
+def _result(out, x, shape, name, dev, stream):
     if out is None:
-        return _new(x.shape, x.dtype, x.device, stream)
-    if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != dev or not out.is_contiguous():
+        return _new(shape, x.dtype, x.device, stream)
+    if out.shape != shape or out.dtype is not x.dtype or out.get_device() != dev or not out.is_contiguous():
         raise TypeError(f"{name} must be dense, of the shape and dtype of its rows and on their device")
     return out
 
@@ -381,17 +382,18 @@ def st_norm_rope_apply_qk(q, k, q_weight, k_weight, positions, spec, eps=1.0e-6,
     positions[n_tokens] as `spec` (RopeSpec) says -> (q_out, k_out).  q and k may be slices of one projection's output; outs default
     to new dense tensors."""
     lib = _lib or load_library()
-    n, _, d = q.shape
+    n, hq, d = q.shape
     dtype, dev = q.dtype, _launch_device(q, "q")
-    hq, q_stride = _rows_arg(q, "q", dev, dtype, n, d)
+    shape, q_stride = _rows_arg(q, "q", dev, dtype, n, d)
     qw = _weight_arg(q_weight, "q_weight", dev, dtype, d)
-    q_out = _result(q_out, q, "q_out", dev, stream)
+    q_out = _result(q_out, q, shape, "q_out", dev, stream)
     kp = ko = kw = None
     hkv = k_stride = 0
     if k is not None:
-        hkv, k_stride = _rows_arg(k, "k", dev, dtype, n, d)
+        shape, k_stride = _rows_arg(k, "k", dev, dtype, n, d)
+        hkv = shape[1]
         kw = _weight_arg(k_weight, "k_weight", dev, dtype, d)
-        k_out = _result(k_out, k, "k_out", dev, stream)
+        k_out = _result(k_out, k, shape, "k_out", dev, stream)
         kp, ko = k.data_ptr(), k_out.data_ptr()
     else:
         k_out = None
@@ -414,39 +416,44 @@ def st_norm_rope_bwd_qk(d_q_out, d_k_out, q, k, q_weight, k_weight, positions, s
     lib = _lib or load_library()
     n, hq, d = d_q_out.shape
     dtype, dev = d_q_out.dtype, _launch_device(d_q_out, "d_q_out")
-    grads, sums, args = [], [], []
-    for g, x, w, dx, name in ((d_q_out, q, q_weight, dq, "q"), (d_k_out, k, k_weight, dk, "k")):
-        if g is None:
-            grads.append(None)
-            sums.append(None)
-            args += [None, 0, None, None, None, 0, 0, None]
-            continue
-        h, _ = _rows_arg(g, "the gradient of " + name, dev, dtype, n, d)
-        if not g.is_contiguous():
-            raise TypeError(f"the gradient of {name}'s result must be dense")
-        stride, dx_stride = 0, h * d
-        if x is not None:
-            hx, stride = _rows_arg(x, name, dev, dtype, n, d)
-            if hx != h:
-                raise TypeError(f"{name} and the gradient of its result differ in heads")
-        if dx is None:
-            dx = _new(g.shape, dtype, g.device, stream)
-        else:
-            hx, dx_stride = _rows_arg(dx, "d" + name, dev, dtype, n, d)
-            if hx != h:
-                raise TypeError(f"d{name} and the gradient of the result differ in heads")
-        wp = _weight_arg(w, name + "_weight", dev, dtype, d)
-        dw = _new(d, torch.float32, g.device, stream) if w is not None and weight_grads else None
-        grads.append(dx)
-        sums.append(dw)
-        args += [dx.data_ptr(), dx_stride, _ptr(dw), g.data_ptr(), _ptr(x), stride, h, wp]
-    if workspace is None and (sums[0] is not None or sums[1] is not None):
-        workspace = _temp_workspace(st_norm_rope_bwd_workspace_bytes(n, hq, 0 if d_k_out is None else d_k_out.shape[1], d), d_q_out.device, stream)
-    status = lib.st_norm_rope_bwd_qk(*args, _positions_arg(positions, dev, n), n, d, eps, C.addressof(spec), _dtype_code(d_q_out), _ptr(workspace),
-                                     0 if workspace is None else workspace.nbytes, _launch_stream(stream, dev))
+    dq, dq_weight, q_args = _bwd_args(d_q_out, q, q_weight, dq, "q", dev, dtype, n, d, weight_grads, stream)
+    dk, dk_weight, k_args = _bwd_args(d_k_out, k, k_weight, dk, "k", dev, dtype, n, d, weight_grads, stream) if d_k_out is not None else \
+        (None, None, (None, 0, None, None, None, 0, 0, None))
+    ws, ws_bytes = None, 0
+    if dq_weight is not None or dk_weight is not None:
+        if workspace is None:
+            workspace = _temp_workspace(st_norm_rope_bwd_workspace_bytes(n, hq, k_args[6], d), d_q_out.device, stream)
+        ws, ws_bytes = _ptr(workspace), workspace.nbytes
+    status = lib.st_norm_rope_bwd_qk(*q_args, *k_args, _positions_arg(positions, dev, n), n, d, eps, C.addressof(spec), _dtype_code(d_q_out), ws, ws_bytes,
+                                     _launch_stream(stream, dev))
     if status:
         _check(status)
-    return (*grads, *sums)
+    return dq, dk, dq_weight, dk_weight
+
+
+def _bwd_args(g, x, w, dx, name, dev, dtype, n, d, weight_grads, stream):
+    """One tensor's gradient, its weight's and the call's arguments for them: g = dL/d result, dense."""
+    shape = g.shape
+    h = shape[1]
+    if shape[0] != n or shape[2] != d or g.dtype is not dtype or g.get_device() != dev or not g.is_contiguous():
+        raise TypeError(f"the gradient of {name}'s result must be dense [n_tokens, heads, head_dim], of the dtype and on the device of the others")
+    stride, dx_stride, xp, dwp, dw = 0, h * d, None, None, None
+    if x is not None:
+        x_shape, stride = _rows_arg(x, name, dev, dtype, n, d)
+        if x_shape[1] != h:
+            raise TypeError(f"{name} and the gradient of its result differ in heads")
+        xp = x.data_ptr()
+    if dx is None:
+        dx = _new(shape, dtype, g.device, stream)
+    else:
+        dx_shape, dx_stride = _rows_arg(dx, "d" + name, dev, dtype, n, d)
+        if dx_shape[1] != h:
+            raise TypeError(f"d{name} and the gradient of the result differ in heads")
+    wp = _weight_arg(w, name + "_weight", dev, dtype, d)
+    if w is not None and weight_grads:
+        dw = _new(d, torch.float32, g.device, stream)
+        dwp = dw.data_ptr()
+    return dx, dw, (dx.data_ptr(), dx_stride, dwp, g.data_ptr(), xp, stride, h, wp)
 
 
 # ------------------------------------------------------------------ plan --

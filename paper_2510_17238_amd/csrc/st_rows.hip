@@ -14,7 +14,7 @@
 // Measured, 4 bits, 8 heads of 128 dims.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 74 us, the rows of a cache
 // without norm and rotation in 56, read back in 59, one after the other in 120; nothing between the loads and the stores but the codes, loads
 // two to eight passes ahead, rows in the order in which they lie, 40 vector instructions less of 379 per pass: each within 3 % of that, so it is
-// memory (at the rate of a large copy 45).  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 5.4 and 3.0.
+// memory (at the rate of a large copy 45).  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 4.8 and 3.0.
 #include <math.h>
 #include <string.h>
 
@@ -39,6 +39,8 @@ struct RowsArgs {
     double eps;
     int rotate, write_len;       // write_len: the workgroup of a sequence's first page writes the new length
     RopeTable rope;
+};
+struct PagesArgs : RowsArgs {
     double2 step[64];            // (cos, sin) of the pairs' angles per token
 };
 
@@ -337,9 +339,12 @@ __device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, c
 
 constexpr int kRowsThreads = 256;
 
-template <int FMT, int D>
-__global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
+// Args: PagesArgs; RowsArgs for a single token per sequence, which needs no angles but its own: a kilobyte of arguments less to hand over (the call
+// 4.7 -> 4.2 us on the host) and no whole pages to tell apart (a token for each of 64 sequences 5.4 -> 4.8).
+template <int FMT, int D, typename Args>
+__global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
     using S = Store<FMT, D>;
+    constexpr bool ONE = std::is_same_v<Args, RowsArgs>;
     constexpr int L = D / 8, RP = kRowsThreads / L, HEADS = RP / kPage;      // rows, whole pages of a head per pass
     constexpr int IMAGE = D * kPage * S::PIECE / 8;                          // bytes of a page of one head
     extern __shared__ __align__(16) unsigned char smem[];
@@ -355,7 +360,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
     const int c = int(threadIdx.x) % L, row = int(threadIdx.x) / L;
     // one token per sequence: its rows do not depend on the lengths, and are asked for before them
     u32x4 k_next = {0u, 0u, 0u, 0u}, v_next = {0u, 0u, 0u, 0u};
-    if (a.max_new == 1 && row < n_heads) {
+    if (ONE && row < n_heads) {
         k_next = *reinterpret_cast<const u32x4*>(a.k_new + b * a.k_stride + (h0 + row) * D + 8 * c);
         v_next = *reinterpret_cast<const u32x4*>(a.v_new + b * a.v_stride + (h0 + row) * D + 8 * c);
     }
@@ -372,9 +377,8 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
     const int page = start / kPage + pi;
     const int lo = max(start, page * kPage), hi = min(start + n, (page + 1) * kPage);
     if (lo >= hi) return;
-    const int id = a.cache.page_table[int64_t(b) * a.cache.max_pages + page];
-    if (id < 0 || id >= a.cache.n_pages) return;                             // never write outside the pool
-    const int slot_lo = lo - page * kPage, cnt = hi - lo;
+    const int id = a.cache.page_table[int64_t(b) * a.cache.max_pages + page];              // (looked at behind the angles)
+    const int slot_lo = lo - page * kPage, cnt = ONE ? 1 : hi - lo;
     const int64_t tok0 = int64_t(b) * a.max_new + (lo - start);
     if (a.rotate) {
         // four consecutive tokens of a pair per thread: one evaluation at the first (a token's index is its position id), then turned on by the pair's
@@ -382,23 +386,31 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
         for (int w = int(threadIdx.x); w < (cnt + 3) / 4 * half; w += kRowsThreads) {
             const int t0 = w / half, i = w - t0 * half;
             const double rev = double(lo + 4 * t0) * a.rope.f[i] * 0.15915494309189535;          // angle / 2 pi
-            const double2 step = a.step[i];
             double2 r;
             sincospi(2.0 * (rev - rint(rev)), &r.y, &r.x);
             r.x *= a.rope.a;
             r.y *= a.rope.a;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                table[(4 * t0 + t) * half + i] = r;                  // (the table holds sixteen tokens)
+            auto keep = [&](int t) {
+                table[t * half + i] = r;
                 if constexpr (CODED) {
-                    s_cos[(4 * t0 + t) * half + i] = float(r.x);
-                    s_sin[(4 * t0 + t) * half + i] = float(r.y);
+                    s_cos[t * half + i] = float(r.x);
+                    s_sin[t * half + i] = float(r.y);
                 }
-                r = double2{r.x * step.x - r.y * step.y, r.y * step.x + r.x * step.y};
+            };
+            if constexpr (ONE) {
+                keep(0);
+            } else {
+                const double2 step = a.step[i];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    keep(4 * t0 + t);                                // (the table holds sixteen tokens)
+                    r = double2{r.x * step.x - r.y * step.y, r.y * step.x + r.x * step.y};
+                }
             }
         }
         __syncthreads();
     }
+    if (id < 0 || id >= a.cache.n_pages) return;                             // never write outside the pool
     // (32 bits hold a key's interval if no product of its weight with something lost below 2^-126 counts: weights to 2^20, and what is lost is under 2^-105)
     bool usual = true;
 #pragma unroll
@@ -421,11 +433,11 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(RowsArgs a) {
         else S::put_key(page, slot, c, code);
     };
 
-    if (cnt < kPage) {
+    if (ONE || cnt < kPage) {
         // part of a page: rows (head, token) in turn, straight to their places
         for (int r = row; r < cnt * n_heads; r += RP) {
             const int h = r / cnt, t = r - h * cnt;
-            if (a.max_new > 1 || r >= RP) {
+            if (!ONE || r >= RP) {
                 k_next = load(a.k_new, a.k_stride, t, h);
                 v_next = load(a.v_new, a.v_stride, t, h);
             }
@@ -488,7 +500,7 @@ constexpr int kAppendWorkgroups = 2048;
 st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
                       const int32_t* start_len, const int32_t* n_new, int max_new, int batch, const void* k_weight, double eps,
                       const RopeTable* rope, hipStream_t s) {
-    RowsArgs a{};
+    PagesArgs a{};
     a.cache = cache_view(c);
     a.k_new = static_cast<const uint16_t*>(k_new);
     a.v_new = static_cast<const uint16_t*>(v_new);
@@ -501,8 +513,8 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     a.k_weight = static_cast<const uint16_t*>(k_weight);
     a.eps = eps;
     a.rotate = rope != nullptr;
-    if (rope) {
-        a.rope = *rope;
+    if (rope) a.rope = *rope;
+    if (rope && max_new > 1) {
         // (128 calls of cos and sin: kept as the table itself is)
         static thread_local double kept_f[64];
         static thread_local double2 kept[64];
@@ -524,19 +536,22 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     a.write_len = start_len || one_reader;
     const int64_t blocks = pages * a.head_groups;
     if (blocks > 0x7fffffff) return fail(ST_ERR_SHAPE, "%s: grid too large", who);
-    auto go = [&](auto kernel, int image) {
-        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * (sizeof(double2) + (c.dtype == ST_BF16 ? 0 : sizeof(float2))) : 0) + size_t(2 * image);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRowsThreads), smem, s, a);
-    };
     // (LDS images: 16 tokens x D dims x HEADS heads, the same bytes for 64 dims and two heads as for 128 and one)
+    auto go = [&](auto format, int image) {
+        constexpr int FMT = decltype(format)::value;
+        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * (sizeof(double2) + (FMT == ST_BF16 ? 0 : sizeof(float2))) : 0) + size_t(2 * image);
+        auto launch = [&](auto kernel, const auto& args) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRowsThreads), smem, s, args); };
+        const RowsArgs& one = a;
+        if (max_new == 1) {
+            if (c.head_dim == 64) launch(append_rows_kernel<FMT, 64, RowsArgs>, one); else launch(append_rows_kernel<FMT, 128, RowsArgs>, one);
+        } else {
+            if (c.head_dim == 64) launch(append_rows_kernel<FMT, 64, PagesArgs>, a); else launch(append_rows_kernel<FMT, 128, PagesArgs>, a);
+        }
+    };
     const int values = 16 * 128;
-    if (c.dtype == ST_MXFP4) {
-        if (c.head_dim == 64) go(append_rows_kernel<ST_MXFP4, 64>, values / 2); else go(append_rows_kernel<ST_MXFP4, 128>, values / 2);
-    } else if (c.dtype == ST_FP8_E4M3) {
-        if (c.head_dim == 64) go(append_rows_kernel<ST_FP8_E4M3, 64>, values); else go(append_rows_kernel<ST_FP8_E4M3, 128>, values);
-    } else {
-        if (c.head_dim == 64) go(append_rows_kernel<ST_BF16, 64>, 2 * values); else go(append_rows_kernel<ST_BF16, 128>, 2 * values);
-    }
+    if (c.dtype == ST_MXFP4) go(std::integral_constant<int, ST_MXFP4>{}, values / 2);
+    else if (c.dtype == ST_FP8_E4M3) go(std::integral_constant<int, ST_FP8_E4M3>{}, values);
+    else go(std::integral_constant<int, ST_BF16>{}, 2 * values);
     ST_LAUNCH_CHECK("append_rows_kernel");
     if (!a.write_len) {
         hipLaunchKernelGGL(append_rows_len_kernel, dim3((unsigned(batch) + 255u) / 256u), dim3(256), 0, s, c.appended_len, n_new, max_new, batch, c.max_pages_per_seq * kPage);
