@@ -1403,8 +1403,8 @@ static inline bool small_decode(int64_t batch, int hkv, int d, int max_src, int 
 // many short ones would take longer units, 128 of 300 tokens with one of 12,000 72 with 4,096 against 97.)
 // 4-bit caches: a quarter of the bytes per token, so the launch is over four times sooner and its end counts four times as much: 1,024 tokens
 // from 512 such units on, longer ones for 8,192 of them (2,048 with more than 8 rows) -- 16 sequences of up to 8K + 16K tokens, 32 / 8 heads of 128 dims
-// 56 with 1,024, 64 by the rule above; 64 of up to 8K + 24K 265 with 2,048, 268 with 1,024, 284 with 4,096; eight tokens of 64 of up to 8K + 16K 251 with 4,096, 290
-// with 1,024; 32 of 700 + 700 17.6 against 20.4 with 512; 4 of 4K + 8K 20.3 with 1,024, 19.4 with 512.
+// 56 with 1,024, 64 by the rule above; 64 of up to 8K + 24K 265 with 2,048, 268 with 1,024, 284 with 4,096; eight tokens of 64 of up to 8K + 16K 232 with 4,096, 247
+// with 2,048, 272 with 1,024; 32 of 700 + 700 17.6 against 20.4 with 512; 4 of 4K + 8K 20.3 with 1,024, 19.4 with 512.
 // A few sequences are bound by the walk over a unit and not by bandwidth: 256 tokens up to 256 units of 512 (one sequence of 4K
 // tokens: 13.5 against 15.3), 128 up to 32 units (2K tokens: 11.7 against 15.3).
 static inline int decode_unit_tokens(int64_t batch, int hkv, int rows, int max_src, int max_rsn, int pinned, bool fp8 = false, bool fp4 = false) {

@@ -4,7 +4,7 @@
 // A token and KV head are D + D / 16 bytes, 136 at D = 128, against 4 D G flops for the G query rows that share them: bound by HBM, and only just.  A
 // compute unit gets one 16-token page of a head every 220 cycles at 6 TB/s, and everything between the load and the matrix instruction has to fit
 // into that.  Measured, 8 KV heads of 128 dims: 64 sequences of up to 8K + 24K tokens, 4 rows a head: 216 us, 5.8 TB/s; 32 of 2K + up to 6K, 2 rows: 40 us,
-// 4.9 TB/s; 64 of up to 8K + 16K, 32 rows: 241 us, 3.8 TB/s, vector instructions 47 % and matrix instructions 18 % of the time.  The codes are laid out as
+// 4.9 TB/s; 64 of up to 8K + 16K, 32 rows: 222 us, 4.2 TB/s, vector instructions 51 % and matrix instructions 20 % of the time.  The codes are laid out as
 // the matrix instructions want them (st_kv_cache), one 16-byte load per lane, page and tensor:
 //   K: lane (m = slot, g) holds 32 consecutive dims of its token -- one block, one scale.  The k-steps of the product take its four dwords in turn;
 //      the query fragments use the same assignment of dims.
@@ -15,7 +15,7 @@
 // and their scales as they are beside 8-bit ones, the queries as two of these, aligns the products of a step at some 12 bits of the largest: scores
 // were off by 2^-12 of it, more than bf16 operands make.)
 // Three workgroups per compute unit hide the loads: the next step's codes asked for a step ahead, in registers or in two sets in turn, cost a
-// workgroup and were 0 to 10 % slower, 2 % faster for 32 rows alone.
+// workgroup or registers that are not there, and were 0 to 10 % slower.
 #include <algorithm>
 
 #include "st_decode.h"
@@ -196,13 +196,14 @@ struct State4 {
                     for (int i = 0; i < 4; ++i) o[r][db][i] *= alpha;
             }
             const float ref = m[r] > -INFINITY ? -m[r] : 0.f;            // (nothing seen so far, or NaN alone)
+            float even = 0.f, odd = 0.f;
 #pragma unroll
             for (int v = 0; v < OWN; ++v)
 #pragma unroll
                 for (int i = 0; i < 4; i += 2) {
                     const float a = __builtin_amdgcn_exp2f(fmaf(t[r][v][i], scale_log2, ref)), b = __builtin_amdgcn_exp2f(fmaf(t[r][v][i + 1], scale_log2, ref));
-                    l[r] += a;
-                    l[r] += b;
+                    even = v + i == 0 ? a : even + a;
+                    odd = v + i == 0 ? b : odd + b;
                     if constexpr (SORT) {
                         p[r][v][i / 2] = pair_bf16(a, b);
                     } else {
@@ -210,6 +211,8 @@ struct State4 {
                         p[r][v][i + 1] = pair_bf16(b, 0.f);
                     }
                 }
+            l[r] += even + odd;
+            asm volatile("" : "+v"(l[r]));                               // (the sums are formed here, not beside the second product: see decode4_split_kernel)
         }
         if (tok + 64 > len) {
             // slots past the visible length hold anything: their weights are 0, their scales must be finite
@@ -335,6 +338,9 @@ __device__ __forceinline__ void row_limits(int (&limit)[RB], const DecodeArgs& a
     }
 }
 
+// Three waves per SIMD leave 168 registers, and two blocks of rows at D = 128 take all of them.  A value that does not fit is one that each step begins
+// with, and waits for in memory: with the weights kept for their sums until the second product there were four such values, the page ids among
+// them, and a step of eight tokens of 64 sequences of up to 8K + 16K took 246 us, now 229.
 template <int D, int RB, int COPIES>
 __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(DecodeArgs a) {
     constexpr int DB = D / 16;
