@@ -1402,9 +1402,10 @@ static inline bool small_decode(int64_t batch, int hkv, int d, int max_src, int 
 // but 64 of 700 + 700, 16 rows 85 with 512, 69 with a unit for each cache.  (Only the bounds are known here: a few long caches among
 // many short ones would take longer units, 128 of 300 tokens with one of 12,000 72 with 4,096 against 97.)
 // 4-bit caches: a quarter of the bytes per token, so the launch is over four times sooner and its end counts four times as much: 1,024 tokens
-// from 512 such units on, longer ones for 8,192 of them (2,048 with more than 8 rows) -- 16 sequences of up to 8K + 16K tokens, 32 / 8 heads of 128 dims
-// 56 with 1,024, 64 by the rule above; 64 of up to 8K + 24K 265 with 2,048, 268 with 1,024, 284 with 4,096; eight tokens of 64 of up to 8K + 16K 232 with 4,096, 247
-// with 2,048, 272 with 1,024; 32 of 700 + 700 17.6 against 20.4 with 512; 4 of 4K + 8K 20.3 with 1,024, 19.4 with 512.
+// from 512 such units on, 2,048 for 4,096 of those; with more than 8 rows, whose partial results are what counts, 4,096 or 2,048 for 2,048 of them.
+// 32 / 8 heads of 128 dims, 16 sequences of up to 8K + 16K tokens: 56 with 1,024, 64 by the rule above; 32 of up to 8K + 24K 129 with 1,024, 124 with
+// 2,048, 128 with 4,096; 64 of these 240, 223 and 228; 128 of up to 4K + 8K 182, 171 and 169; eight tokens of 64 of up to 8K + 16K 272, 247 and 232; 32 of
+// 700 + 700 17.6 against 20.4 with 512; 4 of 4K + 8K 20.3 with 1,024, 19.4 with 512.
 // A few sequences are bound by the walk over a unit and not by bandwidth: 256 tokens up to 256 units of 512 (one sequence of 4K
 // tokens: 13.5 against 15.3), 128 up to 32 units (2K tokens: 11.7 against 15.3).
 static inline int decode_unit_tokens(int64_t batch, int hkv, int rows, int max_src, int max_rsn, int pinned, bool fp8 = false, bool fp4 = false) {
@@ -1413,8 +1414,8 @@ static inline int decode_unit_tokens(int64_t batch, int hkv, int rows, int max_s
     auto units = [&](int unit) { return batch * hkv * per_head(unit); };
     auto even = [&](int unit) { return 5 * per_head(unit) * std::min(unit, std::max(max_src, max_rsn)) <= 6 * (int64_t(max_src) + max_rsn); };
     if (!fp4 && rows > 16 && units(kChunkLong) >= 192) return kChunkLong;
-    const int64_t enough = fp4 ? (rows > 8 ? 2048 : 8192) : rows > 8 ? 384 : fp8 ? 768 : 2048;
-    for (int unit = kChunkLong; unit > kChunk; unit /= 2)
+    const int64_t enough = fp4 ? (rows > 8 ? 2048 : 4096) : rows > 8 ? 384 : fp8 ? 768 : 2048;
+    for (int unit = fp4 && rows <= 8 ? kChunkLong / 2 : kChunkLong; unit > kChunk; unit /= 2)
         if (units(unit) >= enough && even(unit)) return unit;
     if (fp4 && units(2 * kChunk) >= 512) return 2 * kChunk;
     return units(kChunk) > 256 ? kChunk : units(kChunk) > 32 ? kChunk / 2 : kChunkMin;
