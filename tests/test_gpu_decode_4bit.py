@@ -194,6 +194,70 @@ def test_static_scratch_streams_and_graph(st):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,q_len", [(32, 8, 128, 1), (16, 4, 128, 4), (8, 2, 64, 8), (8, 2, 128, 8)])
+def test_a_captured_step_of_growing_caches(st, hq, hkv, d, q_len):
+    """Rows from the projections into the cache and the decode that sees them, captured once, replayed for step after step: what the same calls
+    give one by one, in caches that end as theirs do.  4, 16 (one launch, more than the default LDS) and 32 rows."""
+    n_src, n_rsn, steps = [40, 130], [9, 64], 5
+    twins = [make(st, 11, 2, hkv, d, 160, 64 + 16 * 5, n_src, n_rsn)[0] for _ in range(2)]
+    g = torch.Generator(device=DEV).manual_seed(12)
+    new = torch.zeros((2, q_len, hq + 2 * hkv, d), dtype=torch.bfloat16, device=DEV)          # a projection's output: queries, keys, values
+    w = (1.0 + 0.2 * torch.randn(d, generator=g, device=DEV)).to(torch.bfloat16)
+    spec, _ = spec_of(st)
+    vis = torch.tensor(n_src, dtype=torch.int32, device=DEV)
+    most = 64 + q_len * steps
+    lens = [torch.tensor(n_rsn, dtype=torch.int32, device=DEV) for _ in range(2)]
+    bufs = [(torch.empty((2 * q_len, hq, d), dtype=torch.bfloat16, device=DEV), torch.empty((2, q_len, hq, d), dtype=torch.bfloat16, device=DEV)) for _ in range(2)]
+    flat = new.view(2 * q_len, hq + 2 * hkv, d)
+
+    def step(i):
+        q, out = bufs[i]
+        before = lens[i]
+        pos = (before[:, None] + torch.arange(q_len, dtype=torch.int32, device=DEV)).reshape(-1)
+        st.st_norm_rope_apply_qk(flat[:, :hq], None, w, None, pos, spec, q_out=q)
+        st.st_kv_append_norm_rope(twins[i], st.ST_REASONING, new[:, :, hq:hq + hkv], new[:, :, hq + hkv:], w, spec, start_len=before)
+        before += q_len
+        st.st_attn_decode_dual(q.view(2, q_len, hq, d), twins[i], vis, before, 130, most, out=out, workspace=ws)
+
+    ws = torch.empty(st.st_decode_workspace_bytes(2, hq, hkv, d, q_len, 130, most), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(0)
+    for turn in range(steps):
+        new.copy_(torch.randn(new.shape, generator=g, device=DEV))
+        step(1)
+        want = bufs[1][1].clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bufs[0][1], want) and bool(torch.isfinite(want).all()), turn
+    a, b = twins[0].reasoning, twins[1].reasoning
+    assert torch.equal(a.k_pool, b.k_pool) and torch.equal(a.v_pool, b.v_pool) and torch.equal(a.k_scale, b.k_scale)
+    assert a.appended_len.tolist() == b.appended_len.tolist() == [n + q_len * steps for n in n_rsn]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vis", [1500, 1501, 1519])
+def test_tokens_stored_beside_a_decode_that_does_not_see_them(st, vis):
+    """On another stream, into the page that the visible tokens end in: no byte is shared with them."""
+    dual, _ = make(st, 15, 4, 8, 128, 1600, 600, [vis] * 4, [600] * 4)
+    q = torch.randn((4, 1, 32, 128), device=DEV).to(torch.bfloat16)
+    ref, _ = decode(st, q, dual, [vis] * 4, [600] * 4)
+    dev = lambda x: torch.tensor([x] * 4, dtype=torch.int32, device=DEV)
+    seen, n, start, n_new = dev(vis), dev(600), dev(vis), torch.tensor([1, 7, 20, 37], dtype=torch.int32, device=DEV)
+    k, v = (torch.randn((4, 37, 8, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    for i in range(40):
+        st.st_kv_append_norm_rope(dual, st.ST_SOURCE, k, v, None, None, n_new=n_new, start_len=start, stream=side)
+        outs.append(st.st_attn_decode_dual(q, dual, seen, n, vis, 600))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref) for o in outs)
+
+
+@pytest.mark.gpu
 def test_pools_past_4_gib(st):
     hkv, d = 8, 128
     n_pages = 2 ** 32 // (d // 2 * hkv * 16) + 9
