@@ -63,7 +63,7 @@ __device__ __forceinline__ bool holds_nothing(float m, float l) { return m == -I
 
 // log-sum-exp merge of the waves' states of `rows` rows into the unit's partial result at row slot `slot`
 template <int D>
-__device__ __forceinline__ void merge_waves(const SplitLds<D>& sm, int rows, const DecodeArgs& a, int64_t slot) {
+__device__ __forceinline__ void merge_waves(const SplitLds<D>& sm, const int& rows, const DecodeArgs& a, int64_t slot) {
     for (int e = int(threadIdx.x) * 4; e < rows * D; e += 64 * kSplitWaves * 4) {
         const int row = e / D, d0 = e % D;
         float m_all = -INFINITY;
@@ -102,7 +102,7 @@ __device__ __forceinline__ int unit_of(unsigned block, int nc) {
 // The states of a workgroup that holds ALL of its rows' tokens -- WP states, [WP][rows][D] un-normalised outputs and [WP][rows] (reference
 // exponent, sum) in LDS, 64 W threads -- merged by log-sum-exp in a fixed order into the finished rows of (sequence b, KV head h).
 template <int D, int W, int WP>
-__device__ __forceinline__ void merge_and_store(const float* sm_o, const float2* sm_ml, const DecodeArgs& a, int b, int h, uint16_t* out, float* lse) {
+__device__ __forceinline__ void merge_and_store(const float* sm_o, const float2* sm_ml, const DecodeArgs& a, int b, int h, uint16_t* __restrict__ out, float* __restrict__ lse) {
     // Merge: a thread takes one dim of a row, two or four where the rows have more than the threads; everything it needs is read at once, and
     // all waves take part.  (State by state, each with a branch, by the threads that had four dims: 2,900 of the workgroup's 15,800 cycles
     // with 4 rows of 128 dims, now 2,000; 36 layers of one token, 32 / 8 heads, 400 cached tokens 298.5 -> 291.5 us.)
