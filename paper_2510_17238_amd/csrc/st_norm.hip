@@ -390,14 +390,19 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(const float* __restrict
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-// Tokens of a step and steps in flight of the backward pass: up to four tokens a step where there are plenty, and at most 1,024 workgroups
-// (four per compute unit) that leave sums for the weights.  16,001 tokens of 24 heads: 65 us, with 512 workgroups 76, with 2,048 69, with two
-// tokens a step 66, with eight 68; 1,801 in fp32: 21 us, with 512 20, with 2,048 25.
+// Tokens of a step and steps in flight of the backward pass: at most 1,024 workgroups (four per compute unit) that leave sums for the weights, and where
+// there are tokens enough, as many in a step as make four passes of the workgroup's threads.  16,001 tokens of 24 heads of 128: 65 us, with 512 workgroups
+// 76, with 2,048 69, with two tokens a step 66, with eight 68; 131,072 of 40: 752, with four tokens instead of two 778; 65,536 of 18 heads of 64: 96, with
+// four instead of eight 106; 100,000 of 3 of 64: 42, with four instead of 32 94; 1,801 of 24 fp32 heads: 21, with 512 workgroups 20, with 2,048 25.
 constexpr int kBwdWorkgroups = 1024;
-inline int bwd_tokens(int64_t n_tokens) { return n_tokens >= 4 * kBwdWorkgroups ? 4 : n_tokens >= 2 * kBwdWorkgroups ? 2 : 1; }
-inline int bwd_workgroups(int64_t n_tokens) {
-    const int64_t steps = (n_tokens + bwd_tokens(n_tokens) - 1) / bwd_tokens(n_tokens);
-    return int(std::min<int64_t>(steps, kBwdWorkgroups));
+inline int bwd_tokens(int64_t n_tokens, int64_t heads, int head_dim) {
+    int tokens = 1;
+    while (tokens < 32 && tokens * heads < 4 * kNormThreads / (head_dim / 8) && n_tokens >= 2 * tokens * kBwdWorkgroups) tokens *= 2;
+    return tokens;
+}
+inline int bwd_workgroups(int64_t n_tokens, int64_t heads, int head_dim) {
+    const int tokens = bwd_tokens(n_tokens, heads, head_dim);
+    return int(std::min<int64_t>((n_tokens + tokens - 1) / tokens, kBwdWorkgroups));
 }
 
 // What both directions ask of the sizes.  (Rows of a workgroup are counted in 32 bits, rows of a call in 64.)
@@ -470,8 +475,8 @@ extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q
 }
 
 extern "C" size_t st_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
-    if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0 || head_dim <= 0) return 0;
-    return size_t(bwd_workgroups(n_tokens)) * 2 * head_dim * sizeof(float);
+    if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0 || (head_dim != 64 && head_dim != 128)) return 0;
+    return size_t(bwd_workgroups(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim)) * 2 * head_dim * sizeof(float);
 }
 
 extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_weight, const void* d_q_out, const void* q, int64_t q_stride,
@@ -521,9 +526,9 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     a.positions = positions;
     a.n_tokens = n_tokens;
     a.eps = float(eps);
-    a.tokens = bwd_tokens(n_tokens);
+    a.tokens = bwd_tokens(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const int blocks = bwd_workgroups(n_tokens);
+    const int blocks = bwd_workgroups(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim);
     if (blocks > 0) {
         const size_t smem = std::max(size_t(a.tokens) * a.rope.rot * sizeof(float), size_t(kNormThreads / 64) * 2 * head_dim * sizeof(float));
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kNormThreads), smem, s, a); };

@@ -109,6 +109,16 @@ def test_forward_and_gradients(st, dtype, n, hq, hkv, d, fused, spec):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,hq,hkv,d,fused,spec", [
+    ("bf16", 33001, 1, 1, 64, True, dict(rotary=32)),               # 32 tokens a step of the backward pass, the last one short
+    ("f32", 17003, 3, 1, 64, False, dict(layout="interleaved")),    # 16
+    ("bf16", 9001, 3, 1, 128, True, dict(rotary=112)),              # 8
+])
+def test_few_heads_of_many_tokens(st, dtype, n, hq, hkv, d, fused, spec):
+    test_forward_and_gradients(st, dtype, n, hq, hkv, d, fused, spec)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d,norm_q,norm_k", [("bf16", 128, False, True), ("f32", 64, True, False), ("bf16", 64, False, False)])
 def test_without_weights(st, dtype, d, norm_q, norm_k):
     q, k, wq, wk, pos = inputs(dtype, 85, 6, 3, d, False, 11)
