@@ -347,13 +347,16 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
     constexpr bool ONE = std::is_same_v<Args, RowsArgs>;
     constexpr int L = D / 8, RP = kRowsThreads / L, HEADS = RP / kPage;      // rows, whole pages of a head per pass
     constexpr int IMAGE = D * kPage * S::PIECE / 8;                          // bytes of a page of one head
+    // In LDS the values of eight dims lie 16 bytes further on per lane: 128 or 256 bytes apart, all lanes of a row would write into two banks, or
+    // one.  (4 bits: a lane's bytes are spread as they are.)
+    constexpr int GAP = FMT == ST_MXFP4 ? 0 : 16, RUN = IMAGE / L, PADDED = IMAGE + GAP * L;
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr bool CODED = FMT != ST_BF16;
     // (cos, sin) times a of sixteen tokens, [16][rot / 2]; the same in 32 bits, each for itself (not for bf16 rows, which are all formed in 64 bits)
     const int half = a.rope.rot / 2, angles = a.rotate ? kPage * half : 0;
     double2* table = reinterpret_cast<double2*>(smem);
     float *s_cos = reinterpret_cast<float*>(table + angles), *s_sin = s_cos + angles;
-    uint8_t* image = reinterpret_cast<uint8_t*>(CODED ? s_sin + angles : s_cos);                 // [2][HEADS][IMAGE]
+    uint8_t* image = reinterpret_cast<uint8_t*>(CODED ? s_sin + angles : s_cos);                 // [2][HEADS][PADDED]
     const int group = int(blockIdx.x) % a.head_groups, pi = (int(blockIdx.x) / a.head_groups) % a.touched, b = int(blockIdx.x) / (a.head_groups * a.touched);
     const int capacity = a.cache.max_pages * kPage;
     const int h0 = group * a.heads, n_heads = min(a.heads, a.cache.n_kv_heads - h0);
@@ -455,7 +458,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
         v_next = load(a.v_new, a.v_stride, t, sub);
     }
     for (int h = 0, turn = 0; h < n_heads; h += HEADS, turn ^= 1) {
-        uint8_t* img = image + turn * (HEADS * IMAGE);
+        uint8_t* img = image + turn * (HEADS * PADDED);
         const int mine = h + sub;
         if (mine < n_heads) {
             const u32x4 k_raw = k_next, v_raw = v_next;
@@ -464,7 +467,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
                 v_next = load(a.v_new, a.v_stride, t, mine + HEADS);
             }
             const int64_t page_head = int64_t(id) * a.cache.n_kv_heads + h0 + mine;
-            put(S::encode(v_raw), true, img + sub * IMAGE, page_head, t);
+            put(S::encode(v_raw), true, img + sub * PADDED + GAP * c, page_head, t);
             put(key(k_raw, t), false, page_of(a.cache.k_pool, mine), page_head, t);
         }
         __syncthreads();
@@ -473,9 +476,10 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
         const int at = int(threadIdx.x) * SHARE;
         if (h + at / IMAGE < n_heads) {
             uint8_t* dst = page_of(a.cache.v_pool, h) + at;
-            if constexpr (SHARE == 16) *reinterpret_cast<u32x4*>(dst) = *reinterpret_cast<const u32x4*>(img + at);
-            else if constexpr (SHARE == 8) *reinterpret_cast<u32x2*>(dst) = *reinterpret_cast<const u32x2*>(img + at);
-            else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(img + at);
+            const uint8_t* src = img + at + GAP * (at / RUN);
+            if constexpr (SHARE == 16) *reinterpret_cast<u32x4*>(dst) = *reinterpret_cast<const u32x4*>(src);
+            else if constexpr (SHARE == 8) *reinterpret_cast<u32x2*>(dst) = *reinterpret_cast<const u32x2*>(src);
+            else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(src);
         }
     }
 }
@@ -536,7 +540,7 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     a.write_len = start_len || one_reader;
     const int64_t blocks = pages * a.head_groups;
     if (blocks > 0x7fffffff) return fail(ST_ERR_SHAPE, "%s: grid too large", who);
-    // (LDS images: 16 tokens x D dims x HEADS heads, the same bytes for 64 dims and two heads as for 128 and one)
+    // (LDS images: 16 tokens x D dims x HEADS heads and the gaps, the same bytes for 64 dims and two heads as for 128 and one)
     auto go = [&](auto format, int image) {
         constexpr int FMT = decltype(format)::value;
         const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * (sizeof(double2) + (FMT == ST_BF16 ? 0 : sizeof(float2))) : 0) + size_t(2 * image);
@@ -550,8 +554,8 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     };
     const int values = 16 * 128;
     if (c.dtype == ST_MXFP4) go(std::integral_constant<int, ST_MXFP4>{}, values / 2);
-    else if (c.dtype == ST_FP8_E4M3) go(std::integral_constant<int, ST_FP8_E4M3>{}, values);
-    else go(std::integral_constant<int, ST_BF16>{}, 2 * values);
+    else if (c.dtype == ST_FP8_E4M3) go(std::integral_constant<int, ST_FP8_E4M3>{}, values + 256);
+    else go(std::integral_constant<int, ST_BF16>{}, 2 * values + 256);
     ST_LAUNCH_CHECK("append_rows_kernel");
     if (!a.write_len) {
         hipLaunchKernelGGL(append_rows_len_kernel, dim3((unsigned(batch) + 255u) / 256u), dim3(256), 0, s, c.appended_len, n_new, max_new, batch, c.max_pages_per_seq * kPage);
