@@ -476,8 +476,8 @@ st_status st_kv_append_rope(const st_dual_cache* caches, st_stream_kind which,
  *                  start + n_new)
  *   k_weight     : bf16 [head_dim], or NULL: keys are not normalised.  eps >= 0 and finite.
  *   spec         : or NULL: keys are not rotated.
- * Keys are normalised and rotated in fp64 and rounded to bf16 once; codes are formed from those bf16 rows (keys under
- * 2^-100 in magnitude may be formed in fp32).  An undefined element of a row of an 8-bit cache is stored as such, beside the
+ * Keys are normalised and rotated in fp64 and rounded to bf16 once; codes are formed from those bf16 rows (in 8- and
+ * 4-bit caches keys under 2^-90 in magnitude may be formed in fp32).  An undefined element of a row of an 8-bit cache is stored as such, beside the
  * codes of the others.  As with st_kv_append, no byte of a token that is not new is written, and the call may run concurrently
  * with a decode step that does not see the new ones.
  * ---------------------------------------------------------------------- */

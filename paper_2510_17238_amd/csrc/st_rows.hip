@@ -11,10 +11,10 @@
 // and the same row would not always be stored alike.  Nearly every row's codes are the same at both ends of the interval that 32-bit arithmetic
 // leaves, though, and those rows are done with it (quick_key).
 //
-// Measured, 4 bits, 8 heads of 128 dims.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 74 us, the rows of a cache
+// Measured, 4 bits, 8 heads of 128 dims.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 71 us, the rows of a cache
 // without norm and rotation in 56, read back in 59, one after the other in 120; nothing between the loads and the stores but the codes, loads
-// two to eight passes ahead, rows in the order in which they lie, 40 vector instructions less of 379 per pass: each within 3 % of that, so it is
-// memory (at the rate of a large copy 45).  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 4.8 and 3.0.
+// two to eight passes ahead, rows in the order in which they lie: each within 3 % of that, so it is
+// memory (at the rate of a large copy 45).  32,768 tokens of rows into 16 bits 73 us, 8 bits 66, 4 bits 54; out again 60, 50 and 43.  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 4.8 and 3.0.
 #include <math.h>
 #include <string.h>
 
@@ -104,8 +104,8 @@ __device__ __forceinline__ uint32_t row_top(const u32x4& x) {
 }
 // The smallest k from -100 on with (bf16 bits) top <= m 2^(e + k), m = 1 + m128 / 128; 0 for top = 0
 __device__ __forceinline__ int scale_exponent(uint32_t top, int m128, int e) {
-    if (top == 0) return 0;
-    return max(int(top >> 7) - 127 - e + (int(top & 127u) > m128 ? 1 : 0), kScaleExpLeast);
+    const int k = max(int((top + uint32_t(127 - m128)) >> 7) - 127 - e, kScaleExpLeast);         // (a significand above m carries)
+    return top == 0 ? 0 : k;
 }
 
 // Storage formats.  encode: a lane's eight values (bf16, of dims 8 c ..) as the format's codes, with the scale's exponent; put_*: to the token's place
@@ -175,7 +175,7 @@ struct Store<ST_MXFP4, D> {
     static __device__ __forceinline__ Code encode(const u32x4& x) {
         const uint32_t top = row_top<4>(x);                  // a block of 32 dims: four lanes
         const bool bad = top >= 0x7f80u;
-        const uint32_t biased = uint32_t(bad ? 127 : scale_exponent(top, 64, 2) + 127);          // 6 = 1.5 * 2^2
+        const uint32_t biased = uint32_t(scale_exponent(top, 64, 2) + 127);                      // 6 = 1.5 * 2^2
         const float scale = __uint_as_float(biased << 23);
         uint32_t w = 0;
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), scale, 0);
@@ -264,14 +264,22 @@ __device__ __forceinline__ u32x4 exact_key(const u32x4& raw, const RowsArgs& a, 
     return f64x8_to_bf16(x);
 }
 
+// Where a lane finds the angles of its dims in 32 bits.  Dims past the rotated ones have angles of their own, (1, 0), behind the table, so that
+// no lane has to be told apart; the sines are there with either sign, for the lower and for the upper dims of their pairs.
+struct QuickTurn {
+    int cos_at, cos_step, sin_at, sin_step;      // from the tables' beginnings; from a token to the next
+    float unit;                                  // what a rounding is of (|n_i| + |n_j|), see quick_key
+};
+
 // The same in 32 bits: bf16 rows (lo, hi) between which the row in 64 bits lies, value by value; false if the row's size is not of 32 bits.
-// Roundings, in units of u = 2^-24: the sum of squares 12 and eps, the mean's root half of these and 2 of its own, two products: 11 on a normalised
-// value; cos and sin 1, their products and the sum 2 of |n_i| + |n_j|: 14 a (|n_i| + |n_j|), taken as 20.
+// Roundings, in units of u = 2^-24, of y = r (c n_i + s n_j) with n = x w, which is exact: c and s 1 each, the product and the sum 2, r, which is formed
+// in 64 bits, and the last product 1 each: 5 a r (|n_i| + |n_j|) in all, taken as 6.  (The mean in 32 bits as well, 13: twice as many rows without
+// a single bf16 row between their ends.)
 template <int D>
-__device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const float* cos, const float* sin, u32x4& lo, u32x4& hi) {
+__device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const QuickTurn& turn, int partner, const float* cos, const float* sin,
+                                          u32x4& lo, u32x4& hi) {
     constexpr int L = D / 8;
-    constexpr float kUnits = 20.f / 16777216.f;
-    float x[8], err[8];
+    float x[8], size[8], r = 1.f;
     bool sure = true;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -279,58 +287,52 @@ __device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, c
         x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
     }
     if (a.k_weight) {
-        float ss = 0.f;
+        double ss = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-        const float mean = fmaf(row_sum<L>(ss), 1.f / D, float(a.eps));
-        sure = mean > 0x1p-80f && mean < 0x1p80f;
-        const float r = rsqrtf(mean);
+        for (int i = 0; i < 8; ++i) ss = fma(double(x[i]), double(x[i]), ss);
+        const double mean = fma(row_sum<L>(ss), 1.0 / D, a.eps);
+        sure = mean > 0x1p-60 && mean < 0x1p80;
+        r = float(inverse_root(mean));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[2 * i] = x[2 * i] * r * __uint_as_float(w_raw[i] << 16);
-            x[2 * i + 1] = x[2 * i + 1] * r * __uint_as_float(w_raw[i] & 0xffff0000u);
+            x[2 * i] *= __uint_as_float(w_raw[i] << 16);
+            x[2 * i + 1] *= __uint_as_float(w_raw[i] & 0xffff0000u);
         }
     }
+    if (a.rotate && a.rope.interleaved) {
+        const f32x4 c = *reinterpret_cast<const f32x4*>(cos), s = *reinterpret_cast<const f32x4*>(sin);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) err[i] = kUnits * fabsf(x[i]);
-    if (a.rotate) {
-        const KeyTurn turn(a.rope, int(threadIdx.x) % L);
-        const float unit = kUnits * float(a.rope.a);
-        if (a.rope.interleaved) {
-            if (turn.turned) {
-                const f32x4 c = *reinterpret_cast<const f32x4*>(cos + turn.at), s = *reinterpret_cast<const f32x4*>(sin + turn.at);
+        for (int i = 0; i < 4; ++i) {
+            const float p = x[2 * i], q = x[2 * i + 1];
+            size[2 * i] = size[2 * i + 1] = fabsf(p) + fabsf(q);
+            x[2 * i] = fmaf(p, c[i], -(q * s[i]));
+            x[2 * i + 1] = fmaf(q, c[i], p * s[i]);
+        }
+    } else if (a.rotate) {
+        float other[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = x[2 * i], q = x[2 * i + 1];
-                    err[2 * i] = err[2 * i + 1] = unit * (fabsf(p) + fabsf(q));
-                    x[2 * i] = fmaf(p, c[i], -(q * s[i]));
-                    x[2 * i + 1] = fmaf(q, c[i], p * s[i]);
-                }
-            }
-        } else {
-            float other[8];
+        for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], partner);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], turn.partner);
-            if (turn.turned) {
-                const float sign = turn.high ? 1.f : -1.f;
+        for (int u = 0; u < 2; ++u) {
+            const f32x4 c = *reinterpret_cast<const f32x4*>(cos + 4 * u), s = *reinterpret_cast<const f32x4*>(sin + 4 * u);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const f32x4 c = *reinterpret_cast<const f32x4*>(cos + turn.at + 4 * u), s = *reinterpret_cast<const f32x4*>(sin + turn.at + 4 * u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int e = 4 * u + i;
-                        err[e] = unit * (fabsf(x[e]) + fabsf(other[e]));
-                        x[e] = fmaf(x[e], c[i], other[e] * (sign * s[i]));
-                    }
-                }
+            for (int i = 0; i < 4; ++i) {
+                const int e = 4 * u + i;
+                size[e] = fabsf(x[e]) + fabsf(other[e]);
+                x[e] = fmaf(x[e], c[i], other[e] * s[i]);
             }
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) size[i] = fabsf(x[i]);
     }
+    const float unit = turn.unit * r;
     bf16x8 l, h;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        l[i] = (__bf16)(x[i] - err[i]);
-        h[i] = (__bf16)(x[i] + err[i]);
+        const float err = unit * size[i];
+        l[i] = (__bf16)fmaf(x[i], r, -err);
+        h[i] = (__bf16)fmaf(x[i], r, err);
     }
     lo = __builtin_bit_cast(u32x4, l);
     hi = __builtin_bit_cast(u32x4, h);
@@ -352,11 +354,13 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
     constexpr int GAP = FMT == ST_MXFP4 ? 0 : 16, RUN = IMAGE / L, PADDED = IMAGE + GAP * L;
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr bool CODED = FMT != ST_BF16;
-    // (cos, sin) times a of sixteen tokens, [16][rot / 2]; the same in 32 bits, each for itself (not for bf16 rows, which are all formed in 64 bits)
+    // (cos, sin) times a of sixteen tokens, [16][rot / 2]; in 32 bits the cosines, the sines with either sign, [16][rot], and the angles of dims past
+    // the rotated ones (not for bf16 rows, which are all formed in 64 bits: a fifth of the waves would be, behind the others' longer chain -- 64 sentences
+    // of 64 tokens 15 us, so 19)
     const int half = a.rope.rot / 2, angles = a.rotate ? kPage * half : 0;
     double2* table = reinterpret_cast<double2*>(smem);
-    float *s_cos = reinterpret_cast<float*>(table + angles), *s_sin = s_cos + angles;
-    uint8_t* image = reinterpret_cast<uint8_t*>(CODED ? s_sin + angles : s_cos);                 // [2][HEADS][PADDED]
+    float *s_cos = reinterpret_cast<float*>(table + angles), *s_sin = s_cos + angles, *s_none = s_sin + 2 * angles;
+    uint8_t* image = reinterpret_cast<uint8_t*>(CODED && a.rotate ? s_none + 16 : s_cos);                 // [2][HEADS][PADDED]
     const int group = int(blockIdx.x) % a.head_groups, pi = (int(blockIdx.x) / a.head_groups) % a.touched, b = int(blockIdx.x) / (a.head_groups * a.touched);
     const int capacity = a.cache.max_pages * kPage;
     const int h0 = group * a.heads, n_heads = min(a.heads, a.cache.n_kv_heads - h0);
@@ -397,7 +401,8 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
                 table[t * half + i] = r;
                 if constexpr (CODED) {
                     s_cos[t * half + i] = float(r.x);
-                    s_sin[t * half + i] = float(r.y);
+                    s_sin[t * 2 * half + i] = -float(r.y);
+                    s_sin[t * 2 * half + half + i] = float(r.y);
                 }
             };
             if constexpr (ONE) {
@@ -411,11 +416,21 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
                 }
             }
         }
+        if (CODED && threadIdx.x < 16) s_none[threadIdx.x] = threadIdx.x < 8 ? 1.f : 0.f;
         __syncthreads();
     }
     if (id < 0 || id >= a.cache.n_pages) return;                             // never write outside the pool
-    // (32 bits hold a key's interval if no product of its weight with something lost below 2^-126 counts: weights to 2^20, and what is lost is under 2^-105)
+    QuickTurn quick = {0, 0, 0, 0, 6.f / 16777216.f};
+    int partner = int(threadIdx.x) & 63;
+    // (sizes at which nothing overflows in 32 bits, and what is lost under 2^-126 is under 2^-116 in the key)
     bool usual = true;
+    if (a.rotate) {
+        const KeyTurn turn(a.rope, c);
+        partner = turn.partner;
+        quick = turn.turned ? QuickTurn{turn.at, half, a.rope.interleaved ? half + turn.at : 8 * c, 2 * half, quick.unit * float(a.rope.a)}
+                            : QuickTurn{int(s_none - s_cos), 0, int(s_none + 8 - s_sin), 0, quick.unit};
+        usual = a.rope.a < 0x1p20 && a.rope.a > 0x1p-20;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) usual = usual && (w_raw[i] & 0x7fffu) <= 0x4980u && ((w_raw[i] >> 16) & 0x7fffu) <= 0x4980u;
     auto load = [&](const uint16_t* src, int64_t stride, int t, int h) { return *reinterpret_cast<const u32x4*>(src + (tok0 + t) * stride + (h0 + h) * D + 8 * c); };
@@ -423,10 +438,13 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
     auto key = [&](const u32x4& raw, int t) -> typename S::Code {
         if (!a.k_weight && !a.rotate) return S::encode(raw);
         if constexpr (CODED) {
+            // (the same bf16 row at both ends in four waves of five, the same codes in nearly all others)
             u32x4 x_lo, x_hi;
-            const bool sure = quick_key<D>(raw, a, w_raw, s_cos + t * half, s_sin + t * half, x_lo, x_hi);
-            const typename S::Code c_lo = S::encode(x_lo), c_hi = S::encode(x_hi);
-            if (!__any(!usual || !sure || !S::same(c_lo, c_hi))) return c_lo;          // (seldom otherwise)
+            const bool sure = quick_key<D>(raw, a, w_raw, quick, partner, s_cos + quick.cos_at + t * quick.cos_step, s_sin + quick.sin_at + t * quick.sin_step, x_lo, x_hi) && usual;
+            const uint32_t apart = (x_lo[0] ^ x_hi[0]) | (x_lo[1] ^ x_hi[1]) | (x_lo[2] ^ x_hi[2]) | (x_lo[3] ^ x_hi[3]);
+            const typename S::Code code = S::encode(x_lo);
+            if (!__any(!sure || apart != 0)) return code;
+            if (!__any(!sure || !S::same(code, S::encode(x_hi)))) return code;
         }
         return S::encode(exact_key<D>(raw, a, w_raw, table + t * half));
     };
@@ -543,7 +561,8 @@ st_status append_rows(const char* who, const st_kv_cache& c, const void* k_new, 
     // (LDS images: 16 tokens x D dims x HEADS heads and the gaps, the same bytes for 64 dims and two heads as for 128 and one)
     auto go = [&](auto format, int image) {
         constexpr int FMT = decltype(format)::value;
-        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * (sizeof(double2) + (FMT == ST_BF16 ? 0 : sizeof(float2))) : 0) + size_t(2 * image);
+        const size_t smem = (rope ? size_t(kPage) * (a.rope.rot / 2) * sizeof(double2) : 0) + size_t(2 * image)
+                          + (rope && FMT != ST_BF16 ? (size_t(kPage) * (a.rope.rot / 2) * 3 + 16) * sizeof(float) : 0);
         auto launch = [&](auto kernel, const auto& args) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRowsThreads), smem, s, args); };
         const RowsArgs& one = a;
         if (max_new == 1) {
