@@ -197,6 +197,28 @@ def test_unusual_weights(st):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("attention", [2.0 ** 25, 2.0 ** -25, 0.75])
+@pytest.mark.parametrize("layout,rotary", [("half", 96), ("interleaved", 32), ("half", 128)])
+def test_unusual_attention_factors(st, attention, layout, rotary):
+    """Rotated dims of another size than the others, with a norm and without, in part of a page and in whole ones."""
+    d, n = 128, 39
+    g = gen(12)
+    x = torch.randn((2, n, 3, d), generator=g, device=DEV).to(torch.bfloat16)
+    w = (1.0 + 0.3 * torch.randn(d, generator=g, device=DEV)).to(torch.bfloat16)
+    spec, rope = spec_of(st, rotary=rotary, layout=layout, attention=attention)
+    for store in FORMATS:
+        for weight in (w, None):
+            c, _ = cache_of(st, np.random.default_rng(12), store, 2, 4, 3, d)
+            start = torch.tensor([0, 9], dtype=torch.int32, device=DEV)
+            st.st_kv_append_norm_rope(pair(st, c), st.ST_SOURCE, x, x, weight, spec, eps=1e-6, start_len=start)
+            k = torch.zeros((2, n, 3, d), dtype=torch.bfloat16, device=DEV)
+            st.st_kv_read(pair(st, c), st.ST_SOURCE, k, torch.zeros_like(k), first=start)
+            for b, first in ((0, 0), (1, 9)):
+                want = L.norm_rope(f64(x)[b], f64(weight) if weight is not None else None, np.arange(first, first + n), 1e-6, *rope)
+                assert np.array_equal(f64(k)[b], stored(store, L.bf16(want))), (store, b)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("store", FORMATS)
 def test_rows_for_more_tokens_than_there_are_pages(st, store):
     """max_new and max_n are strides and bounds: up to the largest number, whatever the page table holds."""
