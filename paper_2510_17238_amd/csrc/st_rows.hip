@@ -326,6 +326,11 @@ __device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, c
 #pragma unroll
         for (int i = 0; i < 8; ++i) size[i] = fabsf(x[i]);
     }
+    if (!a.k_weight) {
+        // (nothing has made these sizes ordinary: past 2^100 a product or the interval's ends might pass 2^128; undefined: not below it)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sure = sure && size[i] < 0x1p100f;
+    }
     const float unit = turn.unit * r;
     bf16x8 l, h;
 #pragma unroll
