@@ -271,7 +271,10 @@ struct QuickTurn {
     float unit;                                  // what a rounding is of (|n_i| + |n_j|), see quick_key
 };
 
-// The same in 32 bits: bf16 rows (lo, hi) between which the row in 64 bits lies, value by value; false if the row's size is not of 32 bits.
+// The same in 32 bits: bf16 rows (lo, hi) between whose MAGNITUDES the row in 64 bits lies, value by value; false if the row's size is not of 32 bits.
+// By magnitude, because a block's scale goes by its largest: k(lo) <= k <= k(hi), and where the scales are equal the codes are as monotone, so equal codes
+// at both ends are the row's.  (By value, the largest of either sign next to one line between two scales would put BOTH ends past it.)  A value that may be
+// of either sign has codes of either sign at its ends, zeros too.
 // Roundings, in units of u = 2^-24, of y = r (c n_i + s n_j) with n = x w, which is exact: c and s 1 each, the product and the sum 2, r, which is formed
 // in 64 bits, and the last product 1 each: 5 a r (|n_i| + |n_j|) in all, taken as 6.  (The mean in 32 bits as well, 13: twice as many rows without
 // a single bf16 row between their ends.)
@@ -335,7 +338,7 @@ __device__ __forceinline__ bool quick_key(const u32x4& raw, const RowsArgs& a, c
     bf16x8 l, h;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float err = unit * size[i];
+        const float err = copysignf(unit * size[i], x[i]);
         l[i] = (__bf16)fmaf(x[i], r, -err);
         h[i] = (__bf16)fmaf(x[i], r, err);
     }
