@@ -153,7 +153,7 @@ typedef struct st_rope_spec {
  *   n_kv_heads = 0 (k, k_out, k_weight ignored): the queries alone, as for a decoding step whose key goes through
  *              st_kv_append_norm_rope.
  *   positions : int32 [n_tokens]; eps >= 0 and finite.  At most 65,536 heads of either kind.
- * fp32 arithmetic (the squares are summed in fp32: values up to 2^60), results rounded once.
+ * fp32 arithmetic, results rounded once; rows whose squares, with eps, fp32 does not hold are scaled by a power of two first.
  * ---------------------------------------------------------------------- */
 st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, int32_t n_q_heads, const void* q_weight,
                                 void* k_out, const void* k, int64_t k_stride, int32_t n_kv_heads, const void* k_weight,

@@ -130,6 +130,8 @@ struct NormArgs {
     int64_t n_tokens;
     int tokens;                      // of a workgroup's step
     float eps;
+    double eps64;                    // for rows that are scaled; half its exponent (far below any row's for eps = 0)
+    int eps_half;
     float* part;                     // backward: [workgroups][2][D] sums for the weights' gradients, or null
     RopeTable rope;
 };
@@ -195,6 +197,29 @@ struct Turn {
     }
 };
 
+// Whether a row's mean square, eps added, leaves it to 32 bits: no square, product or root of a row of this size is lost or overflows.  Other rows -- none
+// where eps is one that models use -- are scaled by a power of two, eps with them: the norm of x 2^-e under eps 2^-2e is the norm of x.
+__device__ __forceinline__ bool ordinary(float mean) { return mean > 0x1p-60f && mean < 0x1p80f; }
+constexpr int kNoSize = -4096;
+// The row's eight dims in a lane times 2^-e, e the exponent of the row's largest or of eps's root; the mean square of those.
+template <int L>
+__device__ __forceinline__ int scale_row(float (&x)[8], const NormArgs& a, float& mean) {
+    float top = 0.f, ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+#pragma unroll
+    for (int o = 1; o < L; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+    int e = max(top > 0.f ? __builtin_amdgcn_frexp_expf(top) : kNoSize, a.eps_half);
+    e = e == kNoSize || top == INFINITY ? 0 : e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = ldexpf(x[i], -e);
+        ss = fmaf(x[i], x[i], ss);
+    }
+    mean = row_sum<L>(ss) * (1.f / (8 * L)) + float(ldexp(a.eps64, -2 * e));
+    return e;
+}
+
 // Forward.  A workgroup takes rows [block * rows, + rows) of the n_tokens * (q_heads + k_heads) rows of both tensors, token by
 // token: few rows (down to one pass) where there are few in all, so that a decoding step's token is one memory round trip.  The next
 // pass's rows are asked for before this one's are worked on.
@@ -250,7 +275,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormArgs a, int
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-            const float rs = rsqrtf(row_sum<L>(ss) * (1.f / D) + a.eps);
+            float mean = row_sum<L>(ss) * (1.f / D) + a.eps;
+            if (!ordinary(mean)) scale_row<L>(x, a, mean);
+            const float rs = rsqrtf(mean);
             float w0[8], w1[8];
             w[0].get(w0);
             w[1].get(w1);
@@ -265,9 +292,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormArgs a, int
 
 // Backward.  Workgroups walk steps of a.tokens tokens, first the query rows of a step, then its key rows, and keep the sums for the
 // weights' gradients in registers; each leaves one partial sum per tensor, added up in a fixed order by weight_sum_kernel.
-// (A step's first rows asked for before its table: bf16 1 % faster, fp32 40 % slower, for want of registers.)
+// (A step's first rows asked for before its table: bf16 1 % faster, fp32 40 % slower, for want of registers.  The four workgroups per compute unit are asked
+// for: fp32 rows take 128 registers and a few spilled ones, with 130 1,801 tokens of 24 heads were 24.8 us instead of 22.)
 template <typename T, int D>
-__global__ __launch_bounds__(kNormThreads) void norm_rope_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(kNormThreads, 4) void norm_rope_bwd_kernel(NormArgs a) {
     constexpr int L = D / 8, RP = kNormThreads / L;
     extern __shared__ __align__(16) float smem[];
     const int half = a.rope.rot / 2, c = int(threadIdx.x) % L, row = int(threadIdx.x) / L;
@@ -319,7 +347,15 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_bwd_kernel(NormArgs a)
                     ss = fmaf(x[i], x[i], ss);
                     sg = fmaf(g[i] * w[i], x[i], sg);
                 }
-                const float rs = rsqrtf(row_sum<L>(ss) * (1.f / D) + a.eps);
+                float mean = row_sum<L>(ss) * (1.f / D) + a.eps;
+                int e = 0;
+                if (!ordinary(mean)) {
+                    e = scale_row<L>(x, a, mean);
+                    sg = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sg = fmaf(g[i] * w[i], x[i], sg);
+                }
+                const float rs = rsqrtf(mean);
                 const float back = row_sum<L>(sg) * (1.f / D) * rs * rs;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -327,6 +363,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_bwd_kernel(NormArgs a)
                     dw[W][i] = fmaf(g[i], xr, dw[W][i]);
                     g[i] = rs * (g[i] * w[i] - x[i] * back);
                 }
+                if (e != 0)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] = ldexpf(g[i], -e);
             }
             Eight<T>::store(static_cast<T*>(t.out) + (tok0 + t_now) * t.out_stride + h_now * D + 8 * c, g);
         }
@@ -405,6 +444,11 @@ inline int bwd_workgroups(int64_t n_tokens, int64_t heads, int head_dim) {
     return int(std::min<int64_t>((n_tokens + tokens - 1) / tokens, kBwdWorkgroups));
 }
 
+inline void set_eps(NormArgs& a, double eps) {
+    a.eps = float(eps);
+    a.eps64 = eps;
+    a.eps_half = eps > 0.0 ? (ilogb(eps) + 2) / 2 : kNoSize;
+}
 // What both directions ask of the sizes.  (Rows of a workgroup are counted in 32 bits, rows of a call in 64.)
 static st_status check_sizes(const char* who, int64_t n_tokens, int n_q_heads, int n_kv_heads, double eps) {
     if (n_tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0) return fail(ST_ERR_INVALID_ARG, "%s: bad sizes", who);
@@ -451,7 +495,7 @@ extern "C" st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q
     }
     a.positions = positions;
     a.n_tokens = n_tokens;
-    a.eps = float(eps);
+    set_eps(a, eps);
     // Rows of a workgroup: one pass of its threads while that makes no more than 1,024 workgroups, else up to four tokens, whose table
     // the heads share.  131,072 tokens of 40 heads: 495 us, one token each 493, sixteen 539; 4,099 of 18 fp32 heads: 9.4 us, with up to 256
     // workgroups 9.5, up to 4,096 10.9, one token each 10.7.
@@ -525,7 +569,7 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     if (dq_weight && dq_weight == dk_weight) return fail(ST_ERR_INVALID_ARG, "%s: dq_weight and dk_weight are one array", who);
     a.positions = positions;
     a.n_tokens = n_tokens;
-    a.eps = float(eps);
+    set_eps(a, eps);
     a.tokens = bwd_tokens(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int blocks = bwd_workgroups(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim);
