@@ -81,7 +81,7 @@ enum { ST_PROF_PREFILL_ATTN = 0, ST_PROF_DECODE_SPLIT = 1, ST_PROF_BWD_DQ = 2, S
        ST_PROF_TILE_PACK = 4, ST_PROF_SOURCE_CHUNK = 5 };
 void st_profile_enable(int32_t on);
 st_status st_profile_repeat(int32_t launches);
-/* Wave timeline of the decode split kernel (<= 16 query rows per sequence and KV head, bf16 caches), for the calling
+/* Wave timeline of the decode split kernel (<= 16 query rows per sequence and KV head of bf16 caches, any of 4-bit caches), for the calling
  * thread's calls while timing is enabled: workgroup i of a launch (four waves: one work unit of one cache of one
  * sequence and KV head, in the order sequence, head, unit, where the units of a head may begin at any of them;
  * units past a cache's length end at once) writes the

@@ -37,6 +37,24 @@ struct DecodeArgs {
     int trace_cap;
 };
 
+// Stamps the workgroup's start and end into the timeline buffer, whichever way the kernel is left.
+struct WaveStamp {
+    unsigned long long* slot;
+    unsigned long long t0;
+    __device__ __forceinline__ WaveStamp(const DecodeArgs& a) : slot(nullptr), t0(0) {
+        if (a.trace && int(blockIdx.x) < a.trace_cap) {
+            slot = a.trace + 2 * size_t(blockIdx.x);
+            t0 = wall_clock64();
+        }
+    }
+    __device__ __forceinline__ ~WaveStamp() {
+        if (slot && threadIdx.x == 0) {
+            slot[0] = t0;
+            slot[1] = wall_clock64();
+        }
+    }
+};
+
 // A barrier for data exchanged through LDS alone: __syncthreads() also waits for every global load in flight -- here the first
 // keys and values, requested before the queries are rotated.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }

@@ -40,24 +40,6 @@ __device__ __forceinline__ u32x4 key_load(const T* p) {
     return *reinterpret_cast<const u32x4*>(p);
 }
 
-// Stamps the workgroup's start and end into the timeline buffer, whichever way the kernel is left.
-struct WaveStamp {
-    unsigned long long* slot;
-    unsigned long long t0;
-    __device__ __forceinline__ WaveStamp(const DecodeArgs& a) : slot(nullptr), t0(0) {
-        if (a.trace && int(blockIdx.x) < a.trace_cap) {
-            slot = a.trace + 2 * size_t(blockIdx.x);
-            t0 = wall_clock64();
-        }
-    }
-    __device__ __forceinline__ ~WaveStamp() {
-        if (slot && threadIdx.x == 0) {
-            slot[0] = t0;
-            slot[1] = wall_clock64();
-        }
-    }
-};
-
 // Fused query rotation (Sec. 3.2, stream-local position ids): fragments j and j + KS/2 of a lane hold the two halves of
 // eight rotation pairs, head dims STRIDE j + off + e and D/2 + the same; `row` holds (cos, sin) of the pairs at the row's
 // position (rope_table_to_lds).

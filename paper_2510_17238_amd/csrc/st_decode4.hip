@@ -346,6 +346,7 @@ __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(Deco
     constexpr int DB = D / 16;
     // two blocks of rows: query fragments; behind them the (cos, sin) of the q_len query positions; after the loop: SplitLds
     extern __shared__ __align__(16) unsigned char smem_raw[];
+    const WaveStamp stamp(a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nc = a.ncs + a.ncr;
     const unsigned bh = blockIdx.x / unsigned(nc);       // (sequence, KV head)
