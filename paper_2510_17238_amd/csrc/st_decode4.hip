@@ -101,19 +101,22 @@ __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
 
 // Running state of a wave: RB blocks of 16 columns, in base-2 exponent units; column n of block r in the lanes (n, g).
 // Few query rows leave most of the 16 columns of a matrix instruction without a row of their own.  They hold the rows again -- COPIES times 16 / COPIES
-// rows --, and each copy takes the softmax of its share of the step's four pages alone (its weights for the others are 0): the exponentials, which
-// cost four times a multiplication, are not formed twice.  The copies are states of their own and are merged at the end (fold_copies).
-// The reference exponent of a column is its largest score so far: the weight of the largest score is 1, which rounds to itself, and it is the
-// largest weights' rounding that shows in the result.  (Moved only when a score exceeds it by 2^8, the exchange between lanes and the rescale
-// of the accumulator are rare and a step of 64 tokens x 32 rows takes 2 % less time, one of 4 rows the same; the rows' distance from 64 bits
-// is a fifth larger, 2.3e-3 against 1.9e-3 of their norm, 1.7e-3 being the rounding of the result.)  The sum takes the weights before they are
-// rounded.
+// rows --, and each copy takes the softmax of its share of the step's four pages alone: the exponentials, which cost four times a multiplication, are
+// not formed twice.  The copies share one reference exponent and their sums are added up at the end (fold_copies).
+// Weights are the second product's in TWO bf16 parts, the rounded weight and, rounded, what that left: 2^-16 of a weight is lost at most, and the rows
+// are as far from 64 bits as their own rounding takes them (1.63 to 1.66e-3 of their norm).  With the first part alone, 1.76 to 1.99e-3.  The second part costs up to eight
+// rows nothing but some vector instructions: a copy has no weights of the other copies' pages, and there takes the second part of the row's weights
+// from the copy that formed them.  More rows take twice the matrix instructions.  64 sequences of up to 8K + 16K tokens, 4, 8, 16 and 32 rows: 178, 181,
+// 191 and 233 us with one part, 180, 183, 195 and 254 with two.
+// The reference exponent of a column moves only when a score exceeds it by 2^8, so that the exchange between lanes and the rescale of the accumulator
+// are rare (32 rows 263 -> 254, 16 rows 197 -> 195): what the weights' parts leave is relative to the weight, whatever its size.  The sum takes the weights as they are.
 template <int D, int RB, int COPIES>
 struct State4 {
     static constexpr int KS = D / 32, DB = D / 16, G = D / 32;
     static constexpr int ROWS = 16 / COPIES, OWN = 4 / COPIES;             // rows of a block; pages of a step that a column takes
+    static constexpr float kRise = 8.f;
     static constexpr bool QUERIES_IN_LDS = RB > 1;                         // (one copy for the four waves, in fragment order [RB][KS][64 lanes])
-    static constexpr bool SORT = RB > 1;                                   // (see the second product)
+    static constexpr bool SORT = COPIES == 1;                              // (9 rows or more: see the second product)
     bf16x8 q[QUERIES_IN_LDS ? 1 : KS];
     const bf16x8* s_q;
     f32x4 o[RB][DB];
@@ -134,6 +137,12 @@ struct State4 {
         const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
         const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
         return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
+    using By8 = std::integral_constant<int, 0x128>;                        // row_ror:8, row_ror:4
+    using By4 = std::integral_constant<int, 0x124>;
+    template <typename T, typename By>
+    static __device__ __forceinline__ T from(T x, By) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), By::value, 0xf, 0xf, true));
     }
     // 64 tokens from token `tok` of a cache of `len` visible tokens, of which this lane's column of block r sees [0, limit[r]) and every row
     // [0, limit_min)
@@ -176,7 +185,8 @@ struct State4 {
                     for (int i = 0; i < 4; ++i) t[r][v][i] = 16 * v + i < left ? t[r][v][i] : -INFINITY;
             }
         }
-        uint32_t p[RB][OWN][SORT ? 2 : 4];                               // weights as bf16: pairs of slots, or one beside a 0
+        uint32_t p[RB][OWN][SORT ? 2 : 4], rest[RB][OWN][SORT ? 2 : 4];  // both parts of the weights: pairs of slots, or one beside a 0 (rest: of the copy two
+                                                                         // places, or one of two, further on)
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             float mx = -INFINITY;
@@ -185,8 +195,10 @@ struct State4 {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, t[r][v][i]);
             mx *= scale_log2;                                            // (which is positive)
-            if (__any(mx > m[r])) {
-                const float top = fmaxf(column_max(mx), m[r]);
+            if (__any(mx > m[r] + kRise)) {
+                float top = fmaxf(column_max(mx), m[r]);
+                if constexpr (COPIES > 1) top = fmaxf(top, from(top, By8{}));
+                if constexpr (COPIES == 4) top = fmaxf(top, from(top, By4{}));
                 const float alpha = top > -INFINITY ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
                 m[r] = top;
                 l[r] *= alpha;
@@ -205,10 +217,16 @@ struct State4 {
                     even = v + i == 0 ? a : even + a;
                     odd = v + i == 0 ? b : odd + b;
                     if constexpr (SORT) {
-                        p[r][v][i / 2] = pair_bf16(a, b);
+                        const uint32_t w = pair_bf16(a, b);
+                        p[r][v][i / 2] = w;
+                        rest[r][v][i / 2] = pair_bf16(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
                     } else {
-                        p[r][v][i] = pair_bf16(a, 0.f);
-                        p[r][v][i + 1] = pair_bf16(b, 0.f);
+                        auto split = [&](float x, int e) {
+                            p[r][v][e] = pair_bf16(x, 0.f);
+                            rest[r][v][e] = from(pair_bf16(x - __uint_as_float(p[r][v][e] << 16), 0.f), By8{});
+                        };
+                        split(a, i);
+                        split(b, i + 1);
                     }
                 }
             l[r] += even + odd;
@@ -226,9 +244,9 @@ struct State4 {
             }
         }
         // The second product.  A converted dword is one slot with dims 32 gg + m and 32 gg + 16 + m, two k-values of an operand whose columns are both
-        // sets of dims.  Few rows: the weights go in twice, beside a 0 each, for the lower dims and for the upper ones -- twice the matrix
-        // instructions, for which the pipe has the time.  Two blocks of rows (SORT): the dwords of two slots are sorted into an operand of either
-        // set, one more vector instruction per conversion for half the matrix instructions of both blocks.
+        // sets of dims.  Up to 8 rows: the weights go in twice, beside a 0 each, for the lower dims and for the upper ones -- twice the matrix
+        // instructions, for which the pipe has the time.  More rows (SORT): the dwords of two slots are sorted into an operand of either
+        // set, one more vector instruction per conversion for half the matrix instructions, of which the second parts of the weights take as many again.
         if constexpr (SORT) {
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf)
@@ -243,11 +261,14 @@ struct State4 {
                         hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302);
                     }
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        const u32x4 w = {p[r][2 * hf][0], p[r][2 * hf][1], p[r][2 * hf + 1][0], p[r][2 * hf + 1][1]};
-                        o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, w), o[r][2 * gg], 0, 0, 0);
-                        o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, w), o[r][2 * gg + 1], 0, 0, 0);
-                    }
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) {
+                            const auto& x = part == 0 ? p : rest;
+                            const u32x4 w = {x[r][2 * hf][0], x[r][2 * hf][1], x[r][2 * hf + 1][0], x[r][2 * hf + 1][1]};
+                            o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, w), o[r][2 * gg], 0, 0, 0);
+                            o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, w), o[r][2 * gg + 1], 0, 0, 0);
+                        }
                 }
         } else {
 #pragma unroll
@@ -257,7 +278,7 @@ struct State4 {
                 for (int r = 0; r < RB; ++r)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        lo[r][i] = COPIES == 1 || mine == u / OWN ? p[r][u % OWN][i] : 0u;
+                        lo[r][i] = mine == u / OWN ? p[r][u % OWN][i] : COPIES == 2 || (mine ^ 2) == u / OWN ? rest[r][u % OWN][i] : 0u;
                         hi[r][i] = lo[r][i] << 16;
                     }
 #pragma unroll
@@ -276,22 +297,12 @@ struct State4 {
     }
     // The four lanes of a column and the copies of a row merged, in a fixed order; afterwards every lane of a row holds its state.
     __device__ __forceinline__ void fold_copies() {
-        auto from = [](float x, auto ctrl) {
-            return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
-        };
-        using By8 = std::integral_constant<int, 0x128>;                  // row_ror:8, row_ror:4
-        using By4 = std::integral_constant<int, 0x124>;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             l[r] += __shfl_xor(l[r], 16);
             l[r] += __shfl_xor(l[r], 32);
             if constexpr (COPIES > 1) {
-                float top = fmaxf(m[r], from(m[r], By8{}));
-                if constexpr (COPIES == 4) top = fmaxf(top, from(top, By4{}));
-                const float alpha = __builtin_amdgcn_exp2f(m[r] - (top > -INFINITY ? top : 0.f));
-                m[r] = top;
                 auto sum = [&](float x) {
-                    x *= alpha;
                     x += from(x, By8{});
                     if constexpr (COPIES == 4) x += from(x, By4{});
                     return x;
