@@ -144,8 +144,16 @@ struct State4 {
     static __device__ __forceinline__ T from(T x, By) {
         return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), By::value, 0xf, 0xf, true));
     }
+    // the bytes of a word's first n slots (n may be negative or more than four)
+    static __device__ __forceinline__ uint32_t slots_below(int n) {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep |= i < n ? 0xffu << (8 * i) : 0u;
+        return keep;
+    }
     // 64 tokens from token `tok` of a cache of `len` visible tokens, of which this lane's column of block r sees [0, limit[r]) and every row
-    // [0, limit_min)
+    // [0, limit_min).  EACH_LIMIT: see each_limit.
+    template <bool EACH_LIMIT>
     __device__ __forceinline__ void step(Codes<D>& c, int tok, int len, const int (&limit)[RB], int limit_min, float scale_log2) {
         const int lane = int(threadIdx.x) & 63, g = lane >> 4, mine = copy();
         f32x4 s[RB][4], t[RB][OWN];                                      // scores of page u: register i is slot 4 g + i
@@ -236,9 +244,7 @@ struct State4 {
             // slots past the visible length hold anything: their weights are 0, their scales must be finite
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) keep |= tok + 16 * u + 4 * g + i < len ? 0xffu << (8 * i) : 0u;
+                const uint32_t keep = slots_below(len - tok - 16 * u - 4 * g);
 #pragma unroll
                 for (int gg = 0; gg < G; ++gg) c.vs[u][gg] &= keep;
             }
@@ -247,52 +253,73 @@ struct State4 {
         // sets of dims.  Up to 8 rows: the weights go in twice, beside a 0 each, for the lower dims and for the upper ones -- twice the matrix
         // instructions, for which the pipe has the time.  More rows (SORT): the dwords of two slots are sorted into an operand of either
         // set, one more vector instruction per conversion for half the matrix instructions, of which the second parts of the weights take as many again.
-        if constexpr (SORT) {
+        // One of its PIECES, into the accumulators sum(r, 0) of the lower and sum(r, 1) of the upper dims; scales(u): the scale word of page u.
+        constexpr int PIECES = SORT ? 2 : 4;
+        auto multiply = [&](int piece, int gg, auto scales, auto sum) {
+            auto pair = [&](int u, int i) { return fp4_pair(c.v[u][gg], scale_of(scales(u), i), i); };
+            auto add = [&](f32x4& x, const u32x4& v, const u32x4& w) { x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), x, 0, 0, 0); };
+            if constexpr (SORT) {
+                u32x4 lo, hi;                                            // four slots of page 2 piece, four of the next
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                for (int gg = 0; gg < G; ++gg) {
-                    u32x4 lo, hi;                                        // four slots of page 2 hf, four of the next
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int u = 2 * hf + (e >> 1), i = 2 * (e & 1);
-                        const uint32_t a = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i), i), b = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i + 1), i + 1);
-                        lo[e] = __builtin_amdgcn_perm(b, a, 0x05040100);
-                        hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302);
-                    }
-#pragma unroll
-                    for (int part = 0; part < 2; ++part)
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) {
-                            const auto& x = part == 0 ? p : rest;
-                            const u32x4 w = {x[r][2 * hf][0], x[r][2 * hf][1], x[r][2 * hf + 1][0], x[r][2 * hf + 1][1]};
-                            o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, w), o[r][2 * gg], 0, 0, 0);
-                            o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, w), o[r][2 * gg + 1], 0, 0, 0);
-                        }
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t first = pair(2 * piece + (e >> 1), 2 * (e & 1)), second = pair(2 * piece + (e >> 1), 2 * (e & 1) + 1);
+                    lo[e] = __builtin_amdgcn_perm(second, first, 0x05040100);
+                    hi[e] = __builtin_amdgcn_perm(second, first, 0x07060302);
                 }
-        } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                u32x4 lo[RB], hi[RB];
-#pragma unroll
-                for (int r = 0; r < RB; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        lo[r][i] = mine == u / OWN ? p[r][u % OWN][i] : COPIES == 2 || (mine ^ 2) == u / OWN ? rest[r][u % OWN][i] : 0u;
-                        hi[r][i] = lo[r][i] << 16;
-                    }
-#pragma unroll
-                for (int gg = 0; gg < G; ++gg) {
-                    u32x4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = fp4_pair(c.v[u][gg], scale_of(c.vs[u][gg], i), i);
+                for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
-                        o[r][2 * gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo[r]), o[r][2 * gg], 0, 0, 0);
-                        o[r][2 * gg + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi[r]), o[r][2 * gg + 1], 0, 0, 0);
+                        const auto& x = part == 0 ? p[r] : rest[r];
+                        const u32x4 w = {x[2 * piece][0], x[2 * piece][1], x[2 * piece + 1][0], x[2 * piece + 1][1]};
+                        add(sum(r, 0), lo, w);
+                        add(sum(r, 1), hi, w);
                     }
+            } else {
+                u32x4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = pair(piece, i);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    u32x4 lo, hi;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        lo[i] = mine == piece / OWN ? p[r][piece % OWN][i] : COPIES == 2 || (mine ^ 2) == piece / OWN ? rest[r][piece % OWN][i] : 0u;
+                        hi[i] = lo[i] << 16;
+                    }
+                    add(sum(r, 0), v, lo);
+                    add(sum(r, 1), v, hi);
                 }
             }
+        };
+        if constexpr (!EACH_LIMIT) {
+#pragma unroll
+            for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+                for (int gg = 0; gg < G; ++gg) multiply(piece, gg, [&](int u) { return c.vs[u][gg]; }, [&](int r, int side) -> f32x4& { return o[r][2 * gg + side]; });
+        } else {
+            // for every limit in turn, with what lies past it cleared, into the columns that have this limit
+            const bool alike = tok + 64 <= limit_min;
+            for (int seen = alike ? len : limit_min; seen <= len; ++seen)
+#pragma unroll
+                for (int gg = 0; gg < G; ++gg) {
+                    f32x4 x[RB][2];
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        x[r][0] = o[r][2 * gg];
+                        x[r][1] = o[r][2 * gg + 1];
+                    }
+#pragma unroll
+                    for (int piece = 0; piece < PIECES; ++piece)
+                        multiply(piece, gg, [&](int u) { return c.vs[u][gg] & slots_below(seen - tok - 16 * u - 4 * g); }, [&](int r, int side) -> f32x4& { return x[r][side]; });
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            o[r][2 * gg][i] = alike || limit[r] == seen ? x[r][0][i] : o[r][2 * gg][i];
+                            o[r][2 * gg + 1][i] = alike || limit[r] == seen ? x[r][1][i] : o[r][2 * gg + 1][i];
+                        }
+                }
         }
     }
     // The four lanes of a column and the copies of a row merged, in a fixed order; afterwards every lane of a row holds its state.
@@ -349,10 +376,26 @@ __device__ __forceinline__ void row_limits(int (&limit)[RB], const DecodeArgs& a
     }
 }
 
+// Whether a block of the values of tokens first .. len - 1 (at most 31) may hold numbers that 0 times is not 0: a scale byte of 253 or more
+template <int D>
+__device__ __forceinline__ bool values_past_finite(const CacheView& cv, int b, int h, int first, int len) {
+    constexpr int G = D / 32;
+    bool found = false;
+    for (int x = int(threadIdx.x) & 63; x < (len - first) * G; x += 64) {
+        const int tok = first + x / G, slot = tok % kPage, id = cv.page_table[int64_t(b) * cv.max_pages + tok / kPage];
+        const uint8_t* scales = reinterpret_cast<const uint8_t*>(cv.k_scale) + (int64_t(min(max(id, 0), cv.n_pages - 1)) * cv.n_kv_heads + h) * D;
+        found = found || scales[D / 2 + ((slot >> 2) * G + x % G) * 4 + (slot & 3)] >= 253;
+    }
+    return __any(found);
+}
+
 // Three waves per SIMD leave 168 registers, and two blocks of rows at D = 128 take all of them.  A value that does not fit is one that each step begins
 // with, and waits for in memory: with the weights kept for their sums until the second product there were four such values, the page ids among
-// them, and a step of eight tokens of 64 sequences of up to 8K + 16K took 246 us, now 229.
-template <int D, int RB, int COPIES>
+// them, and a step of eight tokens of 64 sequences of up to 8K + 16K took 246 us, without them 229.
+// SEVERAL tokens a step: the last of them are not seen by all rows, whose weights are 0 there, and 0 times a finite value is 0.  Where their blocks of values
+// may hold others the unit is worked on again limit by limit (EACH_LIMIT), which is looked up before the first step: asked within the loop, or with any
+// state in common, that rare way cost the usual one a dozen registers (32 rows 250 -> 294 us; so 250 -> 251).
+template <int D, int RB, int COPIES, bool SEVERAL>
 __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(DecodeArgs a) {
     constexpr int DB = D / 16;
     // two blocks of rows: query fragments; behind them the (cos, sin) of the q_len query positions; after the loop: SplitLds
@@ -370,9 +413,8 @@ __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(Deco
     const int len = min(max(is_src ? a.src_len[b] : a.rsn_len[b], 0), cv.max_pages * kPage);
     if (unit0 >= len) return;
     const int n_steps = (min(len - unit0, a.chunk) - 64 * wave + 64 * kSplitWaves - 1) / (64 * kSplitWaves);
-    int limit[RB];
-    row_limits<RB, COPIES>(limit, a, is_src, len);
     const int limit_min = is_src ? len : min(max(len - a.q_len + 1, 0), len);
+    const bool each_limit = SEVERAL && limit_min < min(len, unit0 + a.chunk) && values_past_finite<D>(cv, b, h, limit_min, len);
     using State = State4<D, RB, COPIES>;
     constexpr int KS = D / 32;
     bf16x8* s_q = reinterpret_cast<bf16x8*>(smem_raw);
@@ -382,41 +424,53 @@ __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(Deco
         rope_table_to_lds<D>(s_rot, len_r - a.q_len, a.q_len, rope_frequency<D>(a.freq), 64 * kSplitWaves);
         lds_barrier();
     }
-    State st(s_q);
     if constexpr (State::QUERIES_IN_LDS) {
         for (int i = wave; i < RB * KS; i += kSplitWaves) s_q[i * 64 + lane] = query_fragment<D, COPIES>(a, b, h, i / KS, i % KS, s_rot);
         lds_barrier();
-    } else {
-#pragma unroll
-        for (int j = 0; j < KS; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, s_rot);
     }
-    const int tok0 = unit0 + 64 * wave;
-    for (int s = 0; s < n_steps; ++s) {
-        Codes<D> codes;
-        pages.load(s, a.n_kv_heads, codes);
-        st.step(codes, tok0 + 64 * kSplitWaves * s, len, limit, limit_min, a.scale_log2);
-    }
-    st.fold_copies();
-    // the waves' states meet in LDS, a block of rows at a time: with both at once (66 KB) a compute unit would hold two workgroups, not three
-    const int n = lane & 15, g = lane >> 4;
+    const int tok0 = unit0 + 64 * wave, n = lane & 15, g = lane >> 4;
     const int64_t slot = ((int64_t(b) * a.n_kv_heads + h) * nc + c) * a.rows;
+    auto work = [&](auto each_limit, const Pages4<D>& pages, int len, int limit_min) {
+        int limit[RB];
+        row_limits<RB, COPIES>(limit, a, is_src, len);
+        State st(s_q);
+        if constexpr (!State::QUERIES_IN_LDS) {
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        __syncthreads();                                // everybody is done with the queries and rotations, with the block before
-        const int rows = min(a.rows - 16 * r, 16);
-        const SplitLds<D> sm(smem_raw, rows);
-        if (n < 16 / COPIES && n < rows) {
-            // lane (n, g), block db, register i  <->  d = 16 db + 4 g + i
-            float* po = sm.o + (wave * rows + n) * D;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[r][db];
-            if (g == 0) {
-                sm.m[wave * rows + n] = st.m[r];
-                sm.l[wave * rows + n] = st.l[r];
-            }
+            for (int j = 0; j < KS; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, s_rot);
         }
-        __syncthreads();
-        merge_waves<D>(sm, rows, a, slot + 16 * r);
+        for (int s = 0; s < n_steps; ++s) {
+            Codes<D> codes;
+            pages.load(s, a.n_kv_heads, codes);
+            st.template step<decltype(each_limit)::value>(codes, tok0 + 64 * kSplitWaves * s, len, limit, limit_min, a.scale_log2);
+        }
+        st.fold_copies();
+        // the waves' states meet in LDS, a block of rows at a time: with both at once (66 KB) a compute unit would hold two workgroups, not three
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            __syncthreads();                            // everybody is done with the queries and rotations, with the block before
+            const int rows = min(a.rows - 16 * r, 16);
+            const SplitLds<D> sm(smem_raw, rows);
+            if (n < 16 / COPIES && n < rows) {
+                // lane (n, g), block db, register i  <->  d = 16 db + 4 g + i
+                float* po = sm.o + (wave * rows + n) * D;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[r][db];
+                if (g == 0) {
+                    sm.m[wave * rows + n] = st.m[r];
+                    sm.l[wave * rows + n] = st.l[r];
+                }
+            }
+            __syncthreads();
+            merge_waves<D>(sm, rows, a, slot + 16 * r);
+        }
+    };
+    // (the same for all waves)
+    if (SEVERAL && each_limit) {
+        int own_b = b, own_len = len, own_min = limit_min;
+        asm volatile("" : "+s"(own_b), "+s"(own_len), "+s"(own_min));
+        work(std::true_type{}, Pages4<D>(cv, own_b, h, lane, unit0 + 64 * wave, kSplitWaves), own_len, own_min);
+    } else {
+        work(std::false_type{}, pages, len, limit_min);
     }
 }
 
@@ -424,7 +478,7 @@ __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(Deco
 // dealt out as in the bf16 kernel: reasoning steps from the first wave up, source steps from the last one down.
 constexpr int kSmallWaves4 = 8;
 
-template <int D, int COPIES>
+template <int D, int COPIES, bool SEVERAL>
 __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(DecodeArgs a, uint16_t* __restrict__ out, float* __restrict__ lse) {
     constexpr int DB = D / 16, W = kSmallWaves4;
     extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -433,36 +487,46 @@ __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(Dec
     float2* sm_rot = sm_ml + W * a.rows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = int(blockIdx.x % unsigned(a.n_kv_heads)), b = int(blockIdx.x / unsigned(a.n_kv_heads));
-    const Pages4<D> pages_s(a.src, b, h, lane, 64 * (W - 1 - wave), W), pages_r(a.rsn, b, h, lane, 64 * wave, W);
+    const Pages4<D> first_s(a.src, b, h, lane, 64 * (W - 1 - wave), W), first_r(a.rsn, b, h, lane, 64 * wave, W);
     const int len_s = min(max(a.src_len[b], 0), a.src.max_pages * kPage), len_r = min(max(a.rsn_len[b], 0), a.rsn.max_pages * kPage);
     const int steps_s = (len_s - 64 * (W - 1 - wave) + 64 * W - 1) / (64 * W), steps_r = (len_r - 64 * wave + 64 * W - 1) / (64 * W);
-    int limit_s[1], limit_r[1];
-    row_limits<1, COPIES>(limit_s, a, true, len_s);
-    row_limits<1, COPIES>(limit_r, a, false, len_r);
     const int limit_min = min(max(len_r - a.q_len + 1, 0), len_r);
-    State4<D, 1, COPIES> st(nullptr);
+    const bool each_limit = SEVERAL && limit_min < len_r && values_past_finite<D>(a.rsn, b, h, limit_min, len_r);
     if (a.rope) {
         rope_table_to_lds<D>(sm_rot, len_r - a.q_len, a.q_len, rope_frequency<D>(a.freq), 64 * W);
         lds_barrier();
     }
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, sm_rot);
-    for (int x = 0; x < steps_r + steps_s; ++x) {
-        const bool r = x < steps_r;
-        const int s = r ? x : x - steps_r;
-        Codes<D> codes;
-        pages_r.load(s, r ? pages_r.my_page : pages_s.my_page, r ? pages_r.k_pool : pages_s.k_pool, r ? pages_r.v_pool : pages_s.v_pool,
-                     r ? pages_r.scales : pages_s.scales, a.n_kv_heads, codes);
-        const int limit[1] = {r ? limit_r[0] : limit_s[0]};
-        st.step(codes, 64 * ((r ? wave : W - 1 - wave) + W * s), r ? len_r : len_s, limit, r ? limit_min : len_s, a.scale_log2);
-    }
-    st.fold_copies();
     const int n = lane & 15, g = lane >> 4;
-    if (n < 16 / COPIES && n < a.rows) {
-        float* po = sm_o + (wave * a.rows + n) * D;
+    auto work = [&](auto each_limit, const Pages4<D>& pages_s, const Pages4<D>& pages_r, int len_s, int len_r, int limit_min) {
+        int limit_s[1], limit_r[1];
+        row_limits<1, COPIES>(limit_s, a, true, len_s);
+        row_limits<1, COPIES>(limit_r, a, false, len_r);
+        State4<D, 1, COPIES> st(nullptr);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[0][db];
-        if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], st.l[0]};
+        for (int j = 0; j < D / 32; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, sm_rot);
+        for (int x = 0; x < steps_r + steps_s; ++x) {
+            const bool r = x < steps_r;
+            const int s = r ? x : x - steps_r;
+            Codes<D> codes;
+            pages_r.load(s, r ? pages_r.my_page : pages_s.my_page, r ? pages_r.k_pool : pages_s.k_pool, r ? pages_r.v_pool : pages_s.v_pool,
+                         r ? pages_r.scales : pages_s.scales, a.n_kv_heads, codes);
+            const int limit[1] = {r ? limit_r[0] : limit_s[0]};
+            st.template step<decltype(each_limit)::value>(codes, 64 * ((r ? wave : W - 1 - wave) + W * s), r ? len_r : len_s, limit, r ? limit_min : len_s, a.scale_log2);
+        }
+        st.fold_copies();
+        if (n < 16 / COPIES && n < a.rows) {
+            float* po = sm_o + (wave * a.rows + n) * D;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[0][db];
+            if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], st.l[0]};
+        }
+    };
+    if (SEVERAL && each_limit) {
+        int own_b = b, own_s = len_s, own_r = len_r, own_min = limit_min;
+        asm volatile("" : "+s"(own_b), "+s"(own_s), "+s"(own_r), "+s"(own_min));
+        work(std::true_type{}, Pages4<D>(a.src, own_b, h, lane, 64 * (W - 1 - wave), W), Pages4<D>(a.rsn, own_b, h, lane, 64 * wave, W), own_s, own_r, own_min);
+    } else {
+        work(std::false_type{}, first_s, first_r, len_s, len_r, limit_min);
     }
     __syncthreads();
     merge_and_store<D, W, W>(sm_o, sm_ml, a, b, h, out, lse);
@@ -483,10 +547,14 @@ st_status launch_decode4(const DecodeArgs& a, int head_dim, int64_t units, hipSt
         if (r == ST_OK) hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(64 * kSplitWaves), smem, s, a);
         return r;
     };
-    if (a.rows <= 4) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 4>) : go(decode4_split_kernel<128, 1, 4>);
-    if (a.rows <= 8) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 2>) : go(decode4_split_kernel<128, 1, 2>);
-    if (a.rows <= 16) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 1>) : go(decode4_split_kernel<128, 1, 1>);
-    return head_dim == 64 ? go(decode4_split_kernel<64, 2, 1>) : go(decode4_split_kernel<128, 2, 1>);
+    auto pick = [&](auto several) -> st_status {
+        constexpr bool S = decltype(several)::value;
+        if (a.rows <= 4) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 4, S>) : go(decode4_split_kernel<128, 1, 4, S>);
+        if (a.rows <= 8) return head_dim == 64 ? go(decode4_split_kernel<64, 1, 2, S>) : go(decode4_split_kernel<128, 1, 2, S>);
+        return head_dim == 64 ? go(decode4_split_kernel<64, 1, 1, S>) : go(decode4_split_kernel<128, 1, 1, S>);
+    };
+    if (a.rows <= 16) return a.q_len == 1 ? pick(std::false_type{}) : pick(std::true_type{});
+    return head_dim == 64 ? go(decode4_split_kernel<64, 2, 1, true>) : go(decode4_split_kernel<128, 2, 1, true>);
 }
 
 st_status launch_decode4_small(const DecodeArgs& a, int head_dim, uint16_t* out, float* lse, hipStream_t s) {
@@ -496,9 +564,13 @@ st_status launch_decode4_small(const DecodeArgs& a, int head_dim, uint16_t* out,
         if (r == ST_OK) hipLaunchKernelGGL(kernel, dim3((unsigned)(a.batch * a.n_kv_heads)), dim3(64 * kSmallWaves4), smem, s, a, out, lse);
         return r;
     };
-    if (a.rows <= 4) return head_dim == 64 ? go(decode4_small_kernel<64, 4>) : go(decode4_small_kernel<128, 4>);
-    if (a.rows <= 8) return head_dim == 64 ? go(decode4_small_kernel<64, 2>) : go(decode4_small_kernel<128, 2>);
-    return head_dim == 64 ? go(decode4_small_kernel<64, 1>) : go(decode4_small_kernel<128, 1>);
+    auto pick = [&](auto several) -> st_status {
+        constexpr bool S = decltype(several)::value;
+        if (a.rows <= 4) return head_dim == 64 ? go(decode4_small_kernel<64, 4, S>) : go(decode4_small_kernel<128, 4, S>);
+        if (a.rows <= 8) return head_dim == 64 ? go(decode4_small_kernel<64, 2, S>) : go(decode4_small_kernel<128, 2, S>);
+        return head_dim == 64 ? go(decode4_small_kernel<64, 1, S>) : go(decode4_small_kernel<128, 1, S>);
+    };
+    return a.q_len == 1 ? pick(std::false_type{}) : pick(std::true_type{});
 }
 
 }  // namespace st
