@@ -19,6 +19,24 @@ struct CacheView {
     float* v_scale;
 };
 
+// the two 4-bit codes of byte `byte` (0 .. 3, a constant once loops are unrolled) as bf16 times the power of two in scale's exponent, all the conversion
+// looks at there (all ones: NaN)
+__device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float scale, int byte) {
+    switch (byte) {
+        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    }
+}
+
+__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
+    bf16x2 r;
+    r[0] = (__bf16)lo;
+    r[1] = (__bf16)hi;
+    return __builtin_bit_cast(uint32_t, r);
+}
+
 st_status check_cache(const st_kv_cache& c, const char* who, const char* which, bool allow_fp8 = false, bool allow_fp4 = false);
 CacheView cache_view(const st_kv_cache& c);
 // One token per sequence into a (checked, bf16) cache at index len_after[b] - 1; the length becomes len_after[b].

@@ -82,23 +82,6 @@ struct Pages4 {
 // byte `i` of a scale word where the conversion looks for its exponent (it takes nothing else of the operand)
 __device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_float(i < 3 ? w << (23 - 8 * i) : w >> 1); }
 
-__device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float scale, int byte) {
-    // (the byte is an immediate of the instruction)
-    switch (byte) {
-        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-    }
-}
-
-__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
-    bf16x2 r;
-    r[0] = (__bf16)lo;
-    r[1] = (__bf16)hi;
-    return __builtin_bit_cast(uint32_t, r);
-}
-
 // Running state of a wave: RB blocks of 16 columns, in base-2 exponent units; column n of block r in the lanes (n, g).
 // Few query rows leave most of the 16 columns of a matrix instruction without a row of their own.  They hold the rows again -- COPIES times 16 / COPIES
 // rows --, and each copy takes the softmax of its share of the step's four pages alone: the exponentials, which cost four times a multiplication, are

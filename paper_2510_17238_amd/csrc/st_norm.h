@@ -16,6 +16,20 @@ struct RopeTable {
 // Checks the spec and forms the table (ST_OK), or says what is wrong with it.
 st_status make_rope_table(const char* who, const st_rope_spec* spec, int head_dim, RopeTable* table);
 
+// A lane's place in a rotation, c the lane's place in its row: the lane that holds the partners of its dims, the first of its pairs, whether any of its
+// dims are rotated, whether they are the second halves of their pairs.
+struct RowTurn {
+    int partner, at;
+    bool turned, high;
+    __device__ __forceinline__ RowTurn(const RopeTable& rope, int c) {
+        const int half = rope.rot / 2;
+        high = 8 * c >= half;
+        turned = 8 * c < rope.rot;
+        partner = (int(threadIdx.x) & 63) + (turned ? (high ? -half / 8 : half / 8) : 0);
+        at = rope.interleaved ? 4 * c : high ? 8 * c - half : 8 * c;
+    }
+};
+
 // A row (one token of one head) lies in D / 8 neighbouring lanes, eight dims each.  Sum over those lanes, by data-parallel
 // moves: neighbours, pairs, halves of eight mirrored, of sixteen mirrored.
 template <int LANES, typename F>

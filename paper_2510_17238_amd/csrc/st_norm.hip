@@ -155,19 +155,13 @@ __device__ __forceinline__ void norm_table(const NormArgs& a, int64_t tok0, int 
     }
 }
 
-// The lane's place in a rotation: which other lane holds the partners of its dims, which entries of the table, which sign.
+// The lane's place in a rotation, and which sign its partners' share has.
 template <int D>
-struct Turn {
-    int partner, at;
+struct Turn : RowTurn {
     float sign;
-    bool turned, interleaved;
-    __device__ __forceinline__ Turn(const RopeTable& rope) {
-        const int c = int(threadIdx.x) % (D / 8), half = rope.rot / 2;
-        const bool high = 8 * c >= half;
-        turned = 8 * c < rope.rot;
+    bool interleaved;
+    __device__ __forceinline__ Turn(const RopeTable& rope) : RowTurn(rope, int(threadIdx.x) % (D / 8)) {
         interleaved = rope.interleaved != 0;
-        partner = (int(threadIdx.x) & 63) + (turned ? (high ? -half / 8 : half / 8) : 0);
-        at = interleaved ? 4 * c : high ? 8 * c - half : 8 * c;
         sign = high ? 1.f : -1.f;
     }
     // x turned by the token's angles (BACK: by their negatives); cos, sin: the token's row of the table

@@ -204,19 +204,6 @@ struct Store<ST_MXFP4, D> {
     }
 };
 
-// The lane's place in a rotation, as in the normalising kernels
-struct KeyTurn {
-    int partner, at;             // the lane that holds the partners of its dims; the first of its pairs
-    bool turned, high;           // any of its dims are rotated; they are the second halves of their pairs
-    __device__ __forceinline__ KeyTurn(const RopeTable& rope, int c) {
-        const int half = rope.rot / 2;
-        high = 8 * c >= half;
-        turned = 8 * c < rope.rot;
-        partner = (int(threadIdx.x) & 63) + (turned ? (high ? -half / 8 : half / 8) : 0);
-        at = rope.interleaved ? 4 * c : high ? 8 * c - half : 8 * c;
-    }
-};
-
 // A key row's eight dims in a lane, normalised and rotated in 64 bits; angles: (cos, sin) times a of the token's pairs
 template <int D>
 __device__ __forceinline__ u32x4 exact_key(const u32x4& raw, const RowsArgs& a, const u32x4& w_raw, const double2* angles) {
@@ -239,7 +226,7 @@ __device__ __forceinline__ u32x4 exact_key(const u32x4& raw, const RowsArgs& a, 
         }
     }
     if (a.rotate) {
-        const KeyTurn turn(a.rope, int(threadIdx.x) % L);
+        const RowTurn turn(a.rope, int(threadIdx.x) % L);
         if (a.rope.interleaved) {
             if (turn.turned) {
 #pragma unroll
@@ -433,7 +420,7 @@ __global__ __launch_bounds__(kRowsThreads) void append_rows_kernel(Args a) {
     // (sizes at which nothing overflows in 32 bits, and what is lost under 2^-126 is under 2^-116 in the key)
     bool usual = true;
     if (a.rotate) {
-        const KeyTurn turn(a.rope, c);
+        const RowTurn turn(a.rope, c);
         partner = turn.partner;
         quick = turn.turned ? QuickTurn{turn.at, half, a.rope.interleaved ? half + turn.at : 8 * c, 2 * half, quick.unit * float(a.rope.a)}
                             : QuickTurn{int(s_none - s_cos), 0, int(s_none + 8 - s_sin), 0, quick.unit};
@@ -602,22 +589,8 @@ struct ReadArgs {
     int heads, head_groups;
 };
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    bf16x2 r;
-    r[0] = (__bf16)lo;
-    r[1] = (__bf16)hi;
-    return __builtin_bit_cast(uint32_t, r);
-}
-// the two codes of byte `byte` as bf16 times the power of two of an E8M0 byte (255: NaN), which the conversion reads in the exponent's place
-__device__ __forceinline__ uint32_t pair_of_codes(uint32_t w, uint32_t scale, int byte) {
-    const float s = __uint_as_float(scale << 23);
-    switch (byte) {
-        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
-        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
-    }
-}
+// the two codes of byte `byte` as bf16 times the power of two of an E8M0 byte (255: NaN)
+__device__ __forceinline__ uint32_t pair_of_codes(uint32_t w, uint32_t scale, int byte) { return fp4_pair(w, __uint_as_float(scale << 23), byte); }
 
 // What a thread reads of a page of one head, ahead of its use: a share of the values (eight, at (slot, dim) of its own) and the eight dims 8 c .. of
 // the key of its slot, with their scales.
@@ -686,7 +659,7 @@ struct Stored<ST_FP8_E4M3, D> {
         unpack(k, f);
         u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = pack_bf16(f[2 * i] * ks, f[2 * i + 1] * ks);
+        for (int i = 0; i < 4; ++i) r[i] = pair_bf16(f[2 * i] * ks, f[2 * i + 1] * ks);
         return r;
     }
 };
