@@ -187,9 +187,10 @@ struct State4 {
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, t[r][v][i]);
             mx *= scale_log2;                                            // (which is positive)
             if (__any(mx > m[r] + kRise)) {
-                float top = fmaxf(column_max(mx), m[r]);
+                float top = column_max(mx);
                 if constexpr (COPIES > 1) top = fmaxf(top, from(top, By8{}));
                 if constexpr (COPIES == 4) top = fmaxf(top, from(top, By4{}));
+                top = top > m[r] + kRise ? top : m[r];                   // (a column's own scores alone: no row's bits depend on another's)
                 const float alpha = top > -INFINITY ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
                 m[r] = top;
                 l[r] *= alpha;

@@ -51,3 +51,23 @@ def test_tokens_that_a_row_does_not_see(st, q_len, hq, hkv, d, n_src, n_rsn, uni
         st.st_kv_append_norm_rope(dual, st.ST_REASONING, old_k, old_v, None, None, start_len=at)
         again, again_l = decode(st, q, dual, [n_src] * 2, [n_rsn] * 2, unit_tokens=unit)
         assert torch.equal(again, clean) and torch.equal(again_l, clean_l)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q_len,hq,hkv,d", [(2, 1, 1, 128), (4, 2, 1, 64), (8, 4, 2, 128), (8, 8, 2, 128)])
+@pytest.mark.parametrize("n_src,n_rsn", [(33, 100), (700, 1500)])
+def test_no_bit_of_a_row_depends_on_later_tokens(st, q_len, hq, hkv, d, n_src, n_rsn):
+    """The last token's key replaced by ones that score higher and higher for the last row: the other rows stay as they are, bit by bit."""
+    g = torch.Generator(device=DEV).manual_seed(62)
+    dual, _ = make(st, 62, 2, hkv, d, n_src, n_rsn, [n_src] * 2, [n_rsn] * 2)
+    q = torch.randn((2, q_len, hq, d), generator=g, device=DEV).to(torch.bfloat16)
+    at = torch.tensor([n_rsn - 1] * 2, dtype=torch.int32, device=DEV)
+    ref = None
+    for size in (0.25, 4.0, 16.0, 64.0, 1024.0):
+        k = (size * torch.randn((2, 1, hkv, d), generator=g, device=DEV)).to(torch.bfloat16)
+        st.st_kv_append_norm_rope(dual, st.ST_REASONING, k, k, None, None, start_len=at)
+        out, lse = decode(st, q, dual, [n_src] * 2, [n_rsn] * 2)
+        if ref is not None:
+            assert torch.equal(out[:, :-1], ref[0][:, :-1]) and torch.equal(lse[:, :-1], ref[1][:, :-1]), size
+            assert not torch.equal(out[:, -1], ref[0][:, -1])
+        ref = out, lse
