@@ -104,7 +104,8 @@ struct State4 {
     const bf16x8* s_q;
     f32x4 o[RB][DB];
     float m[RB], l[RB];
-    __device__ __forceinline__ explicit State4(const bf16x8* lds) : s_q(lds) {
+    __device__ __forceinline__ explicit State4(const bf16x8* lds) : s_q(lds) { clear(); }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             m[r] = -INFINITY;
@@ -135,7 +136,7 @@ struct State4 {
         return keep;
     }
     // 64 tokens from token `tok` of a cache of `len` visible tokens, of which this lane's column of block r sees [0, limit[r]) and every row
-    // [0, limit_min).  EACH_LIMIT: see each_limit.
+    // [0, limit_min).  EACH_LIMIT: see decode4_split_kernel.
     template <bool EACH_LIMIT>
     __device__ __forceinline__ void step(Codes<D>& c, int tok, int len, const int (&limit)[RB], int limit_min, float scale_log2) {
         const int lane = int(threadIdx.x) & 63, g = lane >> 4, mine = copy();
@@ -306,6 +307,17 @@ struct State4 {
                 }
         }
     }
+    // Whether any sum is infinite or undefined (0 times it is undefined)
+    __device__ __forceinline__ bool past_finite() const {
+        float none = 0.f;
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) none = fmaf(o[r][db][i], 0.f, none);
+        return __any(none != 0.f);
+    }
     // The four lanes of a column and the copies of a row merged, in a fixed order; afterwards every lane of a row holds its state.
     __device__ __forceinline__ void fold_copies() {
 #pragma unroll
@@ -377,8 +389,9 @@ __device__ __forceinline__ bool values_past_finite(const CacheView& cv, int b, i
 // with, and waits for in memory: with the weights kept for their sums until the second product there were four such values, the page ids among
 // them, and a step of eight tokens of 64 sequences of up to 8K + 16K took 246 us, without them 229.
 // SEVERAL tokens a step: the last of them are not seen by all rows, whose weights are 0 there, and 0 times a finite value is 0.  Where their blocks of values
-// may hold others the unit is worked on again limit by limit (EACH_LIMIT), which is looked up before the first step: asked within the loop, or with any
-// state in common, that rare way cost the usual one a dozen registers (32 rows 250 -> 294 us; so 250 -> 251).
+// may hold others the product is formed limit by limit (EACH_LIMIT).  Here that is looked up before the first step, one more round trip (32 sequences of 2K +
+// 2K tokens, 8 rows 28.5 us, so 30; 64 of up to 8K + 16K 182, 184): asked within the loop, or found in the sums at its end, with any state in common, the
+// rare way costs the usual one registers (32 rows 250 us, with that 262 to 294; 8 rows 192).  One token a step is compiled without any of it.
 template <int D, int RB, int COPIES, bool SEVERAL>
 __global__ __launch_bounds__(64 * kSplitWaves, 3) void decode4_split_kernel(DecodeArgs a) {
     constexpr int DB = D / 16;
@@ -475,17 +488,15 @@ __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(Dec
     const int len_s = min(max(a.src_len[b], 0), a.src.max_pages * kPage), len_r = min(max(a.rsn_len[b], 0), a.rsn.max_pages * kPage);
     const int steps_s = (len_s - 64 * (W - 1 - wave) + 64 * W - 1) / (64 * W), steps_r = (len_r - 64 * wave + 64 * W - 1) / (64 * W);
     const int limit_min = min(max(len_r - a.q_len + 1, 0), len_r);
-    const bool each_limit = SEVERAL && limit_min < len_r && values_past_finite<D>(a.rsn, b, h, limit_min, len_r);
     if (a.rope) {
         rope_table_to_lds<D>(sm_rot, len_r - a.q_len, a.q_len, rope_frequency<D>(a.freq), 64 * W);
         lds_barrier();
     }
-    const int n = lane & 15, g = lane >> 4;
-    auto work = [&](auto each_limit, const Pages4<D>& pages_s, const Pages4<D>& pages_r, int len_s, int len_r, int limit_min) {
+    State4<D, 1, COPIES> st(nullptr);
+    auto walk = [&](auto each_limit, const Pages4<D>& pages_s, const Pages4<D>& pages_r, int b, int len_s, int len_r, int limit_min) {
         int limit_s[1], limit_r[1];
         row_limits<1, COPIES>(limit_s, a, true, len_s);
         row_limits<1, COPIES>(limit_r, a, false, len_r);
-        State4<D, 1, COPIES> st(nullptr);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) st.q[j] = query_fragment<D, COPIES>(a, b, h, 0, j, sm_rot);
         for (int x = 0; x < steps_r + steps_s; ++x) {
@@ -497,20 +508,22 @@ __global__ __launch_bounds__(64 * kSmallWaves4, 2) void decode4_small_kernel(Dec
             const int limit[1] = {r ? limit_r[0] : limit_s[0]};
             st.template step<decltype(each_limit)::value>(codes, 64 * ((r ? wave : W - 1 - wave) + W * s), r ? len_r : len_s, limit, r ? limit_min : len_s, a.scale_log2);
         }
-        st.fold_copies();
-        if (n < 16 / COPIES && n < a.rows) {
-            float* po = sm_o + (wave * a.rows + n) * D;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[0][db];
-            if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], st.l[0]};
-        }
     };
-    if (SEVERAL && each_limit) {
+    walk(std::false_type{}, first_s, first_r, b, len_s, len_r, limit_min);
+    // (SEVERAL, EACH_LIMIT: see decode4_split_kernel.  Here a wave finds in its sums, at no cost, that it has to walk again: looked up before, 0.6 us of 9.)
+    if (SEVERAL && __builtin_expect(limit_min < len_r && 64 * (wave + W * (steps_r - 1)) + 64 > limit_min && st.past_finite(), 0)) {
         int own_b = b, own_s = len_s, own_r = len_r, own_min = limit_min;
         asm volatile("" : "+s"(own_b), "+s"(own_s), "+s"(own_r), "+s"(own_min));
-        work(std::true_type{}, Pages4<D>(a.src, own_b, h, lane, 64 * (W - 1 - wave), W), Pages4<D>(a.rsn, own_b, h, lane, 64 * wave, W), own_s, own_r, own_min);
-    } else {
-        work(std::false_type{}, first_s, first_r, len_s, len_r, limit_min);
+        st.clear();
+        walk(std::true_type{}, Pages4<D>(a.src, own_b, h, lane, 64 * (W - 1 - wave), W), Pages4<D>(a.rsn, own_b, h, lane, 64 * wave, W), own_b, own_s, own_r, own_min);
+    }
+    st.fold_copies();
+    const int n = lane & 15, g = lane >> 4;
+    if (n < 16 / COPIES && n < a.rows) {
+        float* po = sm_o + (wave * a.rows + n) * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db + 4 * g) = st.o[0][db];
+        if (g == 0) sm_ml[wave * a.rows + n] = float2{st.m[0], st.l[0]};
     }
     __syncthreads();
     merge_and_store<D, W, W>(sm_o, sm_ml, a, b, h, out, lse);
