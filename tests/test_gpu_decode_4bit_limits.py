@@ -71,3 +71,23 @@ def test_no_bit_of_a_row_depends_on_later_tokens(st, q_len, hq, hkv, d, n_src, n
             assert torch.equal(out[:, :-1], ref[0][:, :-1]) and torch.equal(lse[:, :-1], ref[1][:, :-1]), size
             assert not torch.equal(out[:, -1], ref[0][:, -1])
         ref = out, lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q_len,hq,hkv,d", [(4, 2, 2, 64), (8, 4, 2, 128), (8, 8, 2, 128)])
+@pytest.mark.parametrize("n_src,n_rsn", [(33, 100), (700, 1500)])
+def test_with_rotated_queries(st, q_len, hq, hkv, d, n_src, n_rsn):
+    """The rotation in the kernel: the angles are still there when a step is gone through limit by limit."""
+    dual, _ = make(st, 63, 2, hkv, d, n_src, n_rsn, [n_src] * 2, [n_rsn] * 2)
+    q = torch.randn((2, q_len, hq, d), generator=torch.Generator(device=DEV).manual_seed(63), device=DEV).to(torch.bfloat16)
+    clean, clean_l = decode(st, q, dual, [n_src] * 2, [n_rsn] * 2, theta_base=1.0e4)
+    at = torch.tensor([n_rsn - 1] * 2, dtype=torch.int32, device=DEV)
+    k, v = (torch.zeros((2, 1, hkv, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    st.st_kv_read(dual, st.ST_REASONING, k, v, first=at)
+    v[1, 0, 0, 40] = float("nan")
+    st.st_kv_append_norm_rope(dual, st.ST_REASONING, k, v, None, None, start_len=at)
+    out, lse = decode(st, q, dual, [n_src] * 2, [n_rsn] * 2, theta_base=1.0e4)
+    group = hq // hkv
+    assert torch.equal(out[:, :-1], clean[:, :-1]) and torch.equal(lse, clean_l) and torch.equal(out[0], clean[0])
+    last = out[1, -1, :group]
+    assert bool(torch.isnan(last[:, 32:64]).all()) and torch.equal(last[:, :32], clean[1, -1, :group, :32]) and torch.equal(last[:, 64:], clean[1, -1, :group, 64:])
