@@ -168,7 +168,8 @@ st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, in
  *   dq_weight, dk_weight : fp32 [head_dim] (written: the sum over all rows), or NULL where it is not wanted; two arrays, also
  *                      where one weight serves both tensors (its gradient is their sum)
  * workspace: at least st_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; not needed (may be NULL) without
- * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine.
+ * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine, in fp32 within a
+ * workgroup (a handful of rows a lane, up to 1,024 workgroups) and in fp64 over the workgroups.
  * With n_tokens = 0 the weight gradients are written as 0. */
 size_t st_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 
@@ -399,7 +400,8 @@ st_status st_attn_prefill_bwd(void* dq, void* dk, void* dv, const void* d_out, c
  *   k_scale: bytes [n_pages][n_kv_heads][head_dim], the scales of keys AND values (cast to float*; v_scale is not used):
  *            [head_dim / 32][16 slots] of the keys, then [slot / 4][head_dim / 32][slot % 4] of the values
  * st_kv_append, st_kv_append_rope, st_kv_append_norm_rope, st_kv_read and st_attn_decode_dual(_rope, _static) accept
- * them; every other call that takes a cache gives ST_ERR_UNSUPPORTED.
+ * them; every other call that takes a cache gives ST_ERR_UNSUPPORTED.  An arriving sentence that has to attend over a 4-bit (or
+ * 8-bit) source cache goes by way of bf16: st_kv_read of the cache, and the prefill attention over those rows.
  * ---------------------------------------------------------------------- */
 typedef struct st_kv_cache {
     void* k_pool;
@@ -493,7 +495,7 @@ st_status st_kv_append_norm_rope(const st_dual_cache* caches, st_stream_kind whi
  * through the prefill attention again.
  *   k_out, v_out : bf16 [batch, max_n, n_kv_heads, head_dim], token first[b] + i in row i.  Rows from n[b] on, tokens past the page
  *                  table and tokens whose page id is outside the pool are left as they were.
- *   first, n     : device int32 [batch]; NULL for 0 and for max_n
+ *   first, n     : device int32 [batch]; NULL for 0 and for max_n.  A first below 0 counts as 0, n is taken into 0 .. max_n.
  * ---------------------------------------------------------------------- */
 st_status st_kv_read(const st_dual_cache* caches, st_stream_kind which, void* k_out, void* v_out, const int32_t* first,
                      const int32_t* n, int32_t max_n, int32_t batch, void* hip_stream);
@@ -517,6 +519,11 @@ st_status st_kv_read(const st_dual_cache* caches, st_stream_kind which, void* k_
  *   max_src_len / max_rsn_len : host upper bounds on the two length vectors (grid size).
  * A row that sees nothing (both lengths 0) gets out = 0, lse = -inf.  Cache slots
  * outside the visible ranges are never used, whatever bit patterns they hold.
+ * Inf and NaN: a key's or value's reach the rows that see its token; in 4-bit caches no others, in bf16 and 8-bit
+ * caches with q_len > 1 a non-finite v of one of the last q_len - 1 tokens may also reach rows of
+ * the step that do not see it (0 x Inf is NaN).
+ * Scores, softmax statistics and sums are fp32.  The softmax weights enter the value product as bf16 (bf16 and 8-bit
+ * caches) or as the sum of two bf16 numbers, which differs from it by 2^-16 of it at most (4-bit caches).
  * workspace: at least st_decode_workspace_bytes(...) bytes, 256-byte aligned.
  * ---------------------------------------------------------------------- */
 typedef struct st_dual_lens {
@@ -564,8 +571,10 @@ st_status st_attn_decode_dual_static(void* out, float* lse, const void* q,
 /* st_attn_decode_dual with the query rotation fused in (Sec. 3.2): q holds UNROTATED
  * queries; row t of sequence b is the reasoning token at index rsn_len[b] - q_len + t of
  * its stream (already appended, Alg. 1), and is rotated by that position id with base
- * theta_base before it is used.  Everything else as for st_attn_decode_dual;
- * theta_base <= 0 gives ST_ERR_INVALID_ARG. */
+ * theta_base before it is used, and rounded to bf16 again.  The rotation is that of st_kv_append_rope (all of head_dim, pairs
+ * (i, i + head_dim / 2), no scaling): where the keys went in through st_kv_append_norm_rope under another
+ * st_rope_spec, the queries have to be rotated by the same spec (st_norm_rope_apply_qk) and this
+ * call is the wrong one.  Everything else as for st_attn_decode_dual; theta_base <= 0 gives ST_ERR_INVALID_ARG. */
 st_status st_attn_decode_dual_rope(void* out, float* lse, const void* q,
                                    const st_dual_cache* caches, const st_dual_lens* lens,
                                    int32_t batch, int32_t n_q_heads, float scale, double theta_base,
@@ -611,7 +620,8 @@ st_status st_attn_decode_dual_append(void* out, float* lse, const void* q, const
  *   max_src_len : host upper bound on src_len
  * The reasoning cache of `caches` is not touched.  The same machinery as the decode step
  * (split over 512-token chunks of the cache, log-sum-exp merge) with the queries cut into
- * blocks of 32 (token, head) rows.
+ * blocks of 32 (token, head) rows.  A non-finite v of one of the chunk's tokens may reach rows of the
+ * chunk before it (0 x Inf is NaN).
  * workspace: at least st_source_chunk_workspace_bytes(...) bytes, 256-byte aligned.
  * ---------------------------------------------------------------------- */
 size_t st_source_chunk_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,

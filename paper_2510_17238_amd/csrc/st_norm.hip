@@ -373,7 +373,8 @@ __global__ __launch_bounds__(kNormThreads, 4) void norm_rope_bwd_kernel(NormArgs
         __syncthreads();
     }
     if (!a.part) return;
-    // the sums of the workgroup's rows: lane groups of a wave first, then the waves, in a fixed order
+    // the sums of the workgroup's rows: lane groups of a wave first, then the waves, in a fixed order.  In 32 bits, as the lanes' own: in 64 the
+    // gradients were 7.2e-8 of their norm from the definition instead of 8.2e-8, and 1,801 tokens of 24 heads in fp32 took 23.4 us instead of 21.1.
     float* s_dw = smem;                                    // [4 waves][2][D]
     const int wave = int(threadIdx.x) / 64, lane = int(threadIdx.x) % 64;
 #pragma unroll

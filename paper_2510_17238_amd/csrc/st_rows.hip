@@ -11,10 +11,11 @@
 // and the same row would not always be stored alike.  Nearly every row's codes are the same at both ends of the interval that 32-bit arithmetic
 // leaves, though, and those rows are done with it (quick_key).
 //
-// Measured, 4 bits, 8 heads of 128 dims.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 71 us, the rows of a cache
+// Measured, 4 bits, 8 heads of 128 dims, calls repeated in a captured graph.  16 documents, 45,630 tokens (187 MB of rows, 50 of codes): stored in 71 us, the rows of a cache
 // without norm and rotation in 56, read back in 59, one after the other in 120; nothing between the loads and the stores but the codes, loads
 // two to eight passes ahead, rows in the order in which they lie: each within 3 % of that, so it is
-// memory (at the rate of a large copy 45).  32,768 tokens of rows into 16 bits 73 us, 8 bits 66, 4 bits 54; out again 60, 50 and 43.  64 sentences of up to 190 tokens: 17 and 9 us; a token for each of 64: 4.8 and 3.0.
+// memory (at the rate of a large copy 45).  32,768 tokens of rows into 16 bits 73 us, 8 bits 66, 4 bits 54; out again 60, 50 and 43.  64 sentences of up to 190 tokens: 18 and
+// 9 us; a token for each of 64: 5.3 and 3.3.
 #include <math.h>
 #include <string.h>
 
