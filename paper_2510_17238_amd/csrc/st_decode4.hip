@@ -91,8 +91,9 @@ __device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_
 // rows nothing but some vector instructions: a copy has no weights of the other copies' pages, and there takes the second part of the row's weights
 // from the copy that formed them.  More rows take twice the matrix instructions.  64 sequences of up to 8K + 16K tokens, 4, 8, 16 and 32 rows: 178, 181,
 // 191 and 233 us with one part, 180, 183, 195 and 254 with two.
-// The reference exponent of a column moves only when a score exceeds it by 2^8, so that the exchange between lanes and the rescale of the accumulator
-// are rare (32 rows 263 -> 254, 16 rows 197 -> 195): what the weights' parts leave is relative to the weight, whatever its size.  The sum takes the weights as they are.
+// The reference exponent of a column moves only when a score exceeds it, and then to 8 above that score, so that the exchange between lanes and the rescale
+// of the accumulator are rare (32 rows 263 -> 254, 16 rows 197 -> 195): what the weights' parts leave is relative to the weight, whatever its size.  No weight is above
+// 1, so that sums of large values stay where the values are.  The sum takes the weights as they are.
 template <int D, int RB, int COPIES>
 struct State4 {
     static constexpr int KS = D / 32, DB = D / 16, G = D / 32;
@@ -187,11 +188,11 @@ struct State4 {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, t[r][v][i]);
             mx *= scale_log2;                                            // (which is positive)
-            if (__any(mx > m[r] + kRise)) {
+            if (__any(mx > m[r])) {
                 float top = column_max(mx);
                 if constexpr (COPIES > 1) top = fmaxf(top, from(top, By8{}));
                 if constexpr (COPIES == 4) top = fmaxf(top, from(top, By4{}));
-                top = top > m[r] + kRise ? top : m[r];                   // (a column's own scores alone: no row's bits depend on another's)
+                top = top > m[r] ? top + kRise : m[r];                   // (a column's own scores alone: no row's bits depend on another's)
                 const float alpha = top > -INFINITY ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
                 m[r] = top;
                 l[r] *= alpha;

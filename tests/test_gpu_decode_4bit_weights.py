@@ -37,3 +37,23 @@ def test_weights_in_full(st, hq, hkv, d, q_len, n_src, n_rsn):
             bound = HALF * np.abs(ref) * (1 + HALF) + (2.0 ** -16 + 2 * delta + 2 * (64 + len(kk) / 16) * U24) * mag * (1 + HALF)
             worst = max(worst, float((np.abs(out[0, t, h] - ref) / bound).max()))
     assert worst <= 1.0, worst
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,q_len", [(2, 2, 128, 1), (4, 1, 64, 1), (8, 2, 128, 4), (16, 1, 128, 1), (8, 2, 128, 8), (17, 1, 64, 1)])
+@pytest.mark.parametrize("n_src,n_rsn", [(512, 256), (512, 2048)])
+def test_large_values_under_rising_scores(st, hq, hkv, d, q_len, n_src, n_rsn):
+    """Values of 2^115 and -2^115, scores that rise by 7.5 powers of two once a wave has seen its first 64 tokens.  Relative to the largest score, all 2,560 of them add up to
+    less than 2^127; relative to the first, 64 of them to more than 2^128.  The result is the value itself: what is lost of weights and sums, below 2^-14, rounds to it or to
+    the next bf16 number below, half a step."""
+    dual, _ = make(st, 5, 1, hkv, d, n_src, n_rsn, [0], [0])
+    sign = torch.where(torch.arange(d, device=DEV) % 3 == 0, -1.0, 1.0)
+    for which, n, first in ((st.ST_SOURCE, n_src, 0), (st.ST_REASONING, n_rsn, 256)):
+        k = torch.zeros((1, n, hkv, d), dtype=torch.bfloat16, device=DEV)
+        k[:, :, :, 0] = (2.0 * (torch.arange(n, device=DEV) % 512 >= first)).to(torch.bfloat16)[None, :, None]
+        v = (sign * 2.0 ** 115).to(torch.bfloat16).expand(1, n, hkv, d).contiguous()
+        st.st_kv_append(dual, which, k, v)
+    q = torch.zeros((1, q_len, hq, d), dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 7.5 / 2 * np.log(2.0) * d ** 0.5
+    out, _ = decode(st, q, dual, [n_src], [n_rsn], unit_tokens=512)
+    assert float((out.double() / (sign.double() * 2.0 ** 115) - 1.0).abs().max()) <= HALF
