@@ -168,8 +168,8 @@ st_status st_norm_rope_apply_qk(void* q_out, const void* q, int64_t q_stride, in
  *   dq_weight, dk_weight : fp32 [head_dim] (written: the sum over all rows), or NULL where it is not wanted; two arrays, also
  *                      where one weight serves both tensors (its gradient is their sum)
  * workspace: at least st_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; not needed (may be NULL) without
- * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine, in fp32 within a
- * workgroup (a handful of rows a lane, up to 1,024 workgroups) and in fp64 over the workgroups.
+ * weight gradients.  Deterministic (no atomics): the sums are formed in an order that the sizes alone determine: fp32 over
+ * the few rows of a lane (up to 1,024 workgroups share the call's), fp64 beyond, where each workgroup's sum is rounded to fp32 once.
  * With n_tokens = 0 the weight gradients are written as 0. */
 size_t st_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 

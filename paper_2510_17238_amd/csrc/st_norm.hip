@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormArgs a, int
 // Backward.  Workgroups walk steps of a.tokens tokens, first the query rows of a step, then its key rows, and keep the sums for the
 // weights' gradients in registers; each leaves one partial sum per tensor, added up in a fixed order by weight_sum_kernel.
 // (A step's first rows asked for before its table: bf16 1 % faster, fp32 40 % slower, for want of registers.  The four workgroups per compute unit are asked
-// for: fp32 rows take 128 registers and a few spilled ones, with 130 1,801 tokens of 24 heads were 24.8 us instead of 22.)
+// for: fp32 rows take 128 registers and a few spilled ones, with 130 1,801 tokens of 24 heads were 24.8 us instead of 22 before the sums below took their present form.)
 template <typename T, int D>
 __global__ __launch_bounds__(kNormThreads, 4) void norm_rope_bwd_kernel(NormArgs a) {
     constexpr int L = D / 8, RP = kNormThreads / L;
@@ -373,25 +373,21 @@ __global__ __launch_bounds__(kNormThreads, 4) void norm_rope_bwd_kernel(NormArgs
         __syncthreads();
     }
     if (!a.part) return;
-    // the sums of the workgroup's rows: lane groups of a wave first, then the waves, in a fixed order.  In 32 bits, as the lanes' own: in 64 the
-    // gradients were 7.2e-8 of their norm from the definition instead of 8.2e-8, and 1,801 tokens of 24 heads in fp32 took 23.4 us instead of 21.1.
-    float* s_dw = smem;                                    // [4 waves][2][D]
-    const int wave = int(threadIdx.x) / 64, lane = int(threadIdx.x) % 64;
+    // the sums of the workgroup's rows over its lane groups, in a fixed order and in 64 bits: a lane has a few rows in 32, and what comes after them adds nothing but the
+    // rounding of the partial sum (16,001 tokens of 24 bf16 heads: gradients 8.8e-8 of their norm from the definition, with shuffles and sums in 32 bits
+    // 10.0e-8; 1,801 tokens in fp32: 7.4e-8 and 8.8e-8, 20.6 and 21.7 us)
+    float* s_dw = smem;                                    // [RP][2][D]
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float v = dw[t][i];
-#pragma unroll
-            for (int o = L; o < 64; o *= 2) v += __shfl_xor(v, o);
-            if (lane < L) s_dw[(wave * 2 + t) * D + 8 * c + i] = v;
-        }
+        for (int u = 0; u < 2; ++u)
+            *reinterpret_cast<f32x4*>(s_dw + (row * 2 + t) * D + 8 * c + 4 * u) = f32x4{dw[t][4 * u], dw[t][4 * u + 1], dw[t][4 * u + 2], dw[t][4 * u + 3]};
     __syncthreads();
     for (int i = int(threadIdx.x); i < 2 * D; i += kNormThreads) {
-        float v = 0.f;
+        double v = 0.0;
 #pragma unroll
-        for (int u = 0; u < kNormThreads / 64; ++u) v += s_dw[u * 2 * D + i];
-        a.part[int64_t(blockIdx.x) * (2 * D) + i] = v;
+        for (int u = 0; u < RP; ++u) v += double(s_dw[u * 2 * D + i]);
+        a.part[int64_t(blockIdx.x) * (2 * D) + i] = float(v);
     }
 }
 
@@ -569,7 +565,7 @@ extern "C" st_status st_norm_rope_bwd_qk(void* dq, int64_t dq_stride, float* dq_
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int blocks = bwd_workgroups(n_tokens, int64_t(n_q_heads) + n_kv_heads, head_dim);
     if (blocks > 0) {
-        const size_t smem = std::max(size_t(a.tokens) * a.rope.rot * sizeof(float), size_t(kNormThreads / 64) * 2 * head_dim * sizeof(float));
+        const size_t smem = std::max(size_t(a.tokens) * a.rope.rot * sizeof(float), size_t(kNormThreads) * 2 * 8 * sizeof(float));
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kNormThreads), smem, s, a); };
         if (dt == ST_F32) {
             if (head_dim == 64) go(norm_rope_bwd_kernel<float, 64>); else go(norm_rope_bwd_kernel<float, 128>);

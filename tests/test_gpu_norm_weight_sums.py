@@ -16,14 +16,14 @@ def st():
 
 def additions(n, heads, all_heads, d):
     """Sums in 32 bits that a row goes through: a lane's rows one after the other (a step's rows are dealt out to the 256 / (d / 8) lane groups, a
-    workgroup of at most 1,024 walks several steps), then the lane groups of a wave in pairs and the four waves."""
+    workgroup of at most 1,024 walks several steps); the lane groups are added up in 64 bits and rounded once."""
     groups = 256 // (d // 8)
     tokens = 1
     while tokens < 32 and tokens * all_heads < 4 * groups and n >= 2 * tokens * 1024:
         tokens *= 2
     steps = -(-n // tokens)
     lane = -(-steps // min(steps, 1024)) * -(-tokens * heads // groups)
-    return lane + int(np.log2(groups // 4)) + 4
+    return lane + 1
 
 
 @pytest.mark.gpu
@@ -45,3 +45,22 @@ def test_every_token_counts(st, dtype, n, hq, hkv, d, fused):
         # without its first or its last token, or the last row of that, the same sum is outside
         for lost in (term[0].sum(0), term[-1].sum(0), term[-1, -1]):
             assert (np.abs(lost) > 2 * bound).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,heads", [(128, 16), (64, 32)])
+def test_small_rows_between_large_ones(st, dtype, d, heads):
+    """One token whose heads are one row for each lane group: gradients 1 and -1 in the first and the last row, 2^-26 between them, x of size 1.  All terms are exact (but
+    for r, one factor of them all), and so is their sum in 64 bits; in 32 a row beside a large one is lost."""
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    sp, _ = spec_of(st, dim=d)
+    sign = torch.where(torch.arange(d, device="cuda") % 3 == 0, -1.0, 1.0)
+    x = sign.expand(1, heads, d).to(t).contiguous()
+    g = torch.full((1, heads, d), 2.0 ** -26, device="cuda")
+    g[0, 0], g[0, -1] = 1.0, -1.0
+    w, pos = torch.ones(d, device="cuda", dtype=t), torch.zeros(1, dtype=torch.int32, device="cuda")
+    _, _, dwq, dwk = st.st_norm_rope_bwd_qk(g.to(t), g.to(t), x, x, w, w, pos, sp, eps=0.0)
+    ref = (heads - 2) * 2.0 ** -26 * f64(sign)
+    for dw in (dwq, dwk):
+        assert (np.abs(f64(dw) - ref) <= 4 * U24 * np.abs(ref)).all(), f64(dw) / ref
