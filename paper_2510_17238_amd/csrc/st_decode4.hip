@@ -3,8 +3,8 @@
 //
 // A token and KV head are D + D / 16 bytes, 136 at D = 128, against 4 D G flops for the G query rows that share them: bound by HBM, and only just.  A
 // compute unit gets one 16-token page of a head every 220 cycles at 6 TB/s, and everything between the load and the matrix instruction has to fit
-// into that.  Measured, 8 KV heads of 128 dims, the least of 40 launches (their mean is 3 to 17 % above): 64 sequences of up to 8K + 24K tokens, 4 rows a
-// head: 215 us, 5.8 TB/s; 32 of 2K + up to 6K, 2 rows: 41 us, 4.9 TB/s; 64 of up to 8K + 16K, 8 tokens of 4 rows: 244 us, 3.8 TB/s, vector instructions 50 %
+// into that.  Measured, 8 KV heads of 128 dims, the least of 40 launches (their mean is 3 to 16 % above): 64 sequences of up to 8K + 24K tokens, 4 rows a
+// head: 217 us, 5.7 TB/s; 32 of 2K + up to 6K, 2 rows: 41 us, 4.9 TB/s; 64 of up to 8K + 16K, 8 tokens of 4 rows: 247 us, 3.7 TB/s, vector instructions 50 %
 // and matrix instructions 27 % of the time.  The codes are laid out as the matrix instructions want them (st_kv_cache), one 16-byte load per lane, page and tensor:
 //   K: lane (m = slot, g) holds 32 consecutive dims of its token -- one block, one scale.  The k-steps of the product take its four dwords in turn;
 //      the query fragments use the same assignment of dims.
